@@ -468,6 +468,75 @@ int csd_gmm_resample(csd_ctx *ctx, int B, int gamma, int C, int cap, const csd_g
                      const int32_t *n_accept, const float *w, const float *xi, const float *v, float *x_new,
                      int32_t *n_prop, uint32_t *flags, int32_t *cap_hits);
 
+/* ---- Categorical (vocabulary) heads -------------------------------------------------------------------
+ * A model whose tokens come from a vocabulary of V entries has explicit distributions too: p and q are softmaxes of logits.
+ * The round is that of the mixture heads with nothing left to approximate: drafts are samples of q, the ratio is p(x) / q(x)
+ * (accept rule of Sec. 3.1, Alg. 1), and max(0, p - q) / Z (Eq. 5) is itself a categorical distribution, so the rejected
+ * position is drawn from it directly, with one uniform and no loop.
+ *
+ * csd_logits: data DEVICE [rows, V], row r at data + r * ld elements, any alignment of rows (0 <= ld); dtype CSD_F32, CSD_BF16 or
+ * CSD_F16; V <= 2^19.  -inf and NaN mask a token; every other value is finite (the type's lowest value is an ordinary, very unlikely
+ * logit; infinity counts as the largest finite fp32 number).
+ * csd_cat_params: DEVICE arrays, one value a row, each or the whole struct NULL = off.  The scaled logit is logit * (1 / temperature),
+ * both rounded to fp32; temperature <= 0 keeps the most likely token (the first of equals) only.  Tokens are ordered by
+ * scaled logit, equals by index.  top_k <= 0 or >= V is off; top_p >= 1 is off, and the most likely token is kept whatever it is;
+ * min_p <= 0 is off, more than 1 counts as 1.  They apply in turn: the top_k first tokens; of these the shortest prefix with at least
+ * top_p of their probability; of these all at least min_p times as likely as the likeliest.
+ * dist: DEVICE float64 [rows, 5], a row's distribution for the calls below: log of the normaliser (of exp(scaled logit) over the kept
+ * tokens), the smallest scaled logit kept, the highest index kept among equals of it, the number of tokens kept, 1 / temperature.
+ * Where every token is masked: -inf, inf, -1, 0.
+ * Sums are 64-bit integers (weights to 2^-44 of the largest): results do not depend on how the work is spread over the device.
+ *
+ *   csd_cat_filter: dist of every row.
+ *   csd_cat_draft_sample: the first token, in index order, whose cumulative probability reaches u[r] in (0,1); -1 where every token is
+ *     masked.  logp device [R] out or NULL: its log probability; dist out or NULL.
+ *   csd_cat_verify: logits_q, dist_q, token [B, gamma] and u [B, gamma] of the drafts; logits_p [B, rows_p] rows with rows_p = gamma, or
+ *     gamma + 1 where the bonus position is evaluated too; dist_p [B * rows_p, 5] out (all rows).  logratio = log p(x) - log q(x): -inf
+ *     where x is not kept by p (or not in [0, V)), inf where it is kept by p only; accept iff log u <= logratio; n_accept, accept_mask
+ *     as csd_verify.  Equal logits and parameters give exactly 0.
+ *   csd_cat_resample: x_new[b] = the token at position n_accept[b], w[b] in (0,1) its uniform: of max(0, p - q) for n_accept < gamma (of p
+ *     where that is nothing), of p at the bonus position; -1 where n_accept = gamma and rows_p = gamma, where n_accept is
+ *     outside [0, rows_p), and where p keeps nothing. */
+typedef struct {
+  const void *data;
+  int dtype;
+  int64_t ld;
+} csd_logits;
+typedef struct {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+} csd_cat_params;
+int csd_cat_filter(csd_ctx *ctx, int R, int V, const csd_logits *logits, const csd_cat_params *params, double *dist);
+int csd_cat_draft_sample(csd_ctx *ctx, int R, int V, const csd_logits *q, const csd_cat_params *params, const float *u, int32_t *token,
+                         float *logp, double *dist);
+int csd_cat_verify(csd_ctx *ctx, int B, int gamma, int rows_p, int V, const csd_logits *q, const double *dist_q, const csd_logits *p,
+                   const csd_cat_params *params_p, const int32_t *token, const float *u, double *dist_p, float *logratio,
+                   int32_t *n_accept, uint32_t *accept_mask);
+int csd_cat_resample(csd_ctx *ctx, int B, int gamma, int rows_p, int V, const csd_logits *q, const double *dist_q, const csd_logits *p,
+                     const double *dist_p, const int32_t *n_accept, const float *w, int32_t *x_new);
+
+/* ---- 8-bit matrices: the norm and the product in front of a vocabulary head ---------------------------
+ * csd_quant: a matrix [rows, K] in 8 bits with a scale for each row and block of 128 columns.  data DEVICE [rows, ld] e4m3, ld = K rounded up
+ * to 128, zeros behind K, 16-byte aligned; scale DEVICE [rows, ls], e8m0 bytes (the block's values are 2^(byte - 127) times its e4m3
+ * numbers; 255 = NaN), ls = ld / 128 rounded up to 4, 127 behind, 4-byte aligned.  csd_quant_pitch (host only) gives ld and ls.
+ *   csd_quantize: x DEVICE [rows, K] of `dtype` (CSD_F32, CSD_BF16, CSD_F16), row r at x + r * ldx.  A block's scale is the smallest power of two
+ *     under which its largest magnitude does not exceed 448; values are rounded to nearest even; a block with an infinity or a NaN becomes NaN.
+ *   csd_norm_quantize: the same of h / sqrt(mean(h^2) + eps) * weight with h = x + residual (residual NULL: x; weight [K] of
+ *     `dtype` or NULL: ones), formed in fp32.  sum [rows, K] of `dtype`, row stride lds, out or NULL: h, rounded; it may be x or
+ *     residual itself (the residual stream is updated in place).
+ *   csd_quant_matmul: out[m, n] = sum_k a[m, k] w[n, k], m < M token rows, n < N vocabulary rows, fp32 accumulation, rounded once to
+ *     `dtype`; out DEVICE, row stride ldo.  Logits for the calls above. */
+typedef struct {
+  uint8_t *data;
+  uint8_t *scale;
+} csd_quant;
+int csd_quant_pitch(int K, int *ld, int *ls);
+int csd_quantize(csd_ctx *ctx, int rows, int K, int dtype, const void *x, int64_t ldx, uint8_t *data, uint8_t *scale);
+int csd_norm_quantize(csd_ctx *ctx, int rows, int K, int dtype, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                      const void *weight, float eps, void *sum, int64_t lds, uint8_t *data, uint8_t *scale);
+int csd_quant_matmul(csd_ctx *ctx, int M, int N, int K, const csd_quant *a, const csd_quant *w, int dtype, void *out, int64_t ldo);
+
 /* Same computation as csd_round, but every array is a HOST pointer: the call copies the inputs
  * to the device, runs the round, copies the outputs back and synchronises before returning. */
 int csd_round_host(csd_ctx *ctx, const csd_head *head_q, const csd_head *head_p,

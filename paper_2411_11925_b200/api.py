@@ -30,7 +30,9 @@ EXPORTS = ("csd_create", "csd_destroy", "csd_last_error", "csd_sync", "csd_launc
            "csd_head_create", "csd_head_destroy", "csd_draft_denoise", "csd_draft_denoise_static", "csd_verify",
            "csd_accept_scan", "csd_resample", "csd_round", "csd_round_host", "csd_draft_denoise_traj",
            "csd_verify_single_path", "csd_verify_unaligned", "csd_bonus_token", "csd_verify_bonus", "csd_round_bonus",
-           "csd_gmm_draft_sample", "csd_gmm_verify", "csd_gmm_resample")
+           "csd_gmm_draft_sample", "csd_gmm_verify", "csd_gmm_resample",
+           "csd_cat_filter", "csd_cat_draft_sample", "csd_cat_verify", "csd_cat_resample",
+           "csd_quant_pitch", "csd_quantize", "csd_norm_quantize", "csd_quant_matmul")
 
 WEIGHT_FIELDS = ("Wz", "bz", "Wt1", "bt1", "Wt2", "bt2", "Win", "bin", "Wada", "bada",
                  "W1", "b1", "W2", "b2", "Wfada", "bfada", "Wout", "bout")
@@ -151,6 +153,21 @@ def lv_ddpm_coefficients(beta: np.ndarray, tau: float = 1.0) -> Dict[str, np.nda
     if rc != 0:
         raise CsdError(rc, "csd_schedule_lv_ddpm: beta must lie in (0, 1) and tau be positive")
     return out
+
+
+def quant_pitch(K: int):
+    """csd_quant_pitch: (ld, ls), the row lengths of an 8-bit matrix's data and scales."""
+    ld, ls = C.c_int(), C.c_int()
+    rc = _LIB.csd_quant_pitch(int(K), C.byref(ld), C.byref(ls))
+    if rc != 0:
+        raise CsdError(rc, "csd_quant_pitch: K must lie in [1, 2^20]")
+    return ld.value, ls.value
+
+
+def quant_empty(rows: int, K: int, device):
+    """(data, scale): room for an 8-bit matrix [rows, K]."""
+    ld, ls = quant_pitch(K)
+    return (torch.empty(rows, ld, dtype=torch.uint8, device=device), torch.empty(rows, ls, dtype=torch.uint8, device=device))
 
 
 def _ptr(t) -> Optional[int]:
@@ -381,6 +398,47 @@ class Context:
 
     def csd_gmm_resample(self, B, gamma, Cdim, cap, q, p, n_accept, w, xi, v, x_new, n_prop, flags, cap_hits):
         rc = _fast.gmm_resample(self._addr, B, gamma, Cdim, cap, q, p, n_accept, w, xi, v, x_new, n_prop, flags, cap_hits)
+        if rc:
+            self._check(rc)
+
+    # Categorical heads.  Logits: device tensors [rows, V] of float32, bfloat16 or float16 with any row stride; params: None or a tuple
+    # (temperature, top_k, top_p, min_p) of device tensors of one value a row (int32 for top_k, else float32) or None;
+    # dist: float64 [rows, 5] (see csd_cat_filter in include/csd.h).
+    def csd_cat_filter(self, R, V, logits, params, dist):
+        rc = _fast.cat_filter(self._addr, self.device, R, V, logits, params, dist)
+        if rc:
+            self._check(rc)
+
+    def csd_cat_draft_sample(self, R, V, logits, params, u, token, logp=None, dist=None):
+        rc = _fast.cat_draft_sample(self._addr, self.device, R, V, logits, params, u, token, logp, dist)
+        if rc:
+            self._check(rc)
+
+    def csd_cat_verify(self, B, gamma, rows_p, V, logits_q, dist_q, logits_p, params_p, token, u, dist_p, logratio, n_accept,
+                       accept_mask=None):
+        rc = _fast.cat_verify(self._addr, self.device, B, gamma, rows_p, V, logits_q, dist_q, logits_p, params_p, token, u, dist_p,
+                              logratio, n_accept, accept_mask)
+        if rc:
+            self._check(rc)
+
+    def csd_cat_resample(self, B, gamma, rows_p, V, logits_q, dist_q, logits_p, dist_p, n_accept, w, x_new):
+        rc = _fast.cat_resample(self._addr, self.device, B, gamma, rows_p, V, logits_q, dist_q, logits_p, dist_p, n_accept, w, x_new)
+        if rc:
+            self._check(rc)
+
+    # 8-bit matrices: (data, scale) as quant_empty gives them
+    def csd_quantize(self, rows, K, x, data, scale):
+        rc = _fast.quantize(self._addr, self.device, rows, K, x, data, scale)
+        if rc:
+            self._check(rc)
+
+    def csd_norm_quantize(self, rows, K, x, residual, weight, eps, sum, data, scale):
+        rc = _fast.norm_quantize(self._addr, self.device, rows, K, x, residual, weight, eps, sum, data, scale)
+        if rc:
+            self._check(rc)
+
+    def csd_quant_matmul(self, M, N, K, a, w, out):
+        rc = _fast.quant_matmul(self._addr, self.device, M, N, K, a, w, out)
         if rc:
             self._check(rc)
 

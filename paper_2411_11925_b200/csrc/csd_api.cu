@@ -23,6 +23,8 @@
 #include "groupchain.cuh"
 #include "widechain.cuh"
 #include "f32chain.cuh"
+#include "cat.cuh"
+#include "quant.cuh"
 
 using namespace csd;
 
@@ -1435,6 +1437,132 @@ int check_verify_dims(csd_ctx* ctx, int B, int gamma, int C) {
   return CSD_OK;
 }
 
+// Kernels of the categorical calls by the types of the draft's and the target's logits.
+template <typename TQ> auto cat_verify_pick_p(int dp) {
+  return dp == CSD_F32 ? cat_verify_kernel<TQ, float> : dp == CSD_BF16 ? cat_verify_kernel<TQ, __nv_bfloat16> : cat_verify_kernel<TQ, __half>;
+}
+auto cat_verify_pick(int dq, int dp) {
+  return dq == CSD_F32 ? cat_verify_pick_p<float>(dp) : dq == CSD_BF16 ? cat_verify_pick_p<__nv_bfloat16>(dp) : cat_verify_pick_p<__half>(dp);
+}
+template <typename TQ> auto cat_resample_pick_p(int dp) {
+  return dp == CSD_F32 ? cat_resample_kernel<TQ, float> : dp == CSD_BF16 ? cat_resample_kernel<TQ, __nv_bfloat16> : cat_resample_kernel<TQ, __half>;
+}
+auto cat_resample_pick(int dq, int dp) {
+  return dq == CSD_F32 ? cat_resample_pick_p<float>(dp) : dq == CSD_BF16 ? cat_resample_pick_p<__nv_bfloat16>(dp) : cat_resample_pick_p<__half>(dp);
+}
+constexpr int kCatMaxV = 1 << 19;        // sums of 2^19 weights of 2^44 stay far below 2^64
+constexpr int kQuantMaxK = 1 << 20;
+
+int check_cat(csd_ctx* ctx, const csd_logits* l, const char* what) {
+  if (!l || !l->data) return fail(ctx, CSD_ERR_INVALID_ARG, "%s logits are null", what);
+  if (l->dtype != CSD_F32 && l->dtype != CSD_BF16 && l->dtype != CSD_F16) return fail(ctx, CSD_ERR_INVALID_ARG, "%s logits have unknown dtype %d", what, l->dtype);
+  if (l->ld < 0) return fail(ctx, CSD_ERR_INVALID_ARG, "%s logits have a negative row stride", what);
+  if (reinterpret_cast<uintptr_t>(l->data) % (l->dtype == CSD_F32 ? 4 : 2)) return fail(ctx, CSD_ERR_INVALID_ARG, "%s logits are not aligned to their type", what);
+  return CSD_OK;
+}
+
+int check_cat_rows(csd_ctx* ctx, int64_t rows, int V) {
+  if (rows < 1 || V < 1) return fail(ctx, CSD_ERR_INVALID_ARG, "row count %lld and vocabulary V = %d must be >= 1", static_cast<long long>(rows), V);
+  if (V > kCatMaxV) return fail(ctx, CSD_ERR_UNSUPPORTED, "vocabulary V = %d exceeds %d", V, kCatMaxV);
+  if (rows > (1 << 27)) return fail(ctx, CSD_ERR_UNSUPPORTED, "row count %lld exceeds 2^27", static_cast<long long>(rows));
+  return CSD_OK;
+}
+
+int check_cat_round(csd_ctx* ctx, int B, int gamma, int rows_p, int V) {
+  if (B < 1 || gamma < 1) return fail(ctx, CSD_ERR_INVALID_ARG, "B = %d and gamma = %d must be >= 1", B, gamma);
+  if (gamma > 32) return fail(ctx, CSD_ERR_UNSUPPORTED, "gamma = %d exceeds 32", gamma);
+  if (rows_p != gamma && rows_p != gamma + 1) return fail(ctx, CSD_ERR_SHAPE, "%d target rows a sequence: gamma = %d or one more (the bonus position) are taken", rows_p, gamma);
+  return check_cat_rows(ctx, static_cast<int64_t>(B) * rows_p, V);
+}
+
+CatView cat_view(const csd_logits* l) { return CatView{l->data, l->ld}; }
+
+// Blocks a row: as many as keep the device's SMs busy with two blocks each, none with less than 4096 tokens of its own.
+int cat_cluster(const csd_ctx* ctx, int64_t rows, int V) {
+  int cs = 1;
+  while (cs < kCatMaxCluster && rows * cs * 2 <= 2 * ctx->num_sms && V > 4096 * cs) cs *= 2;
+  return cs;
+}
+
+template <typename P>
+int launch_cat(csd_ctx* ctx, void (*kern)(P), int64_t rows, int cs, const P& p) {
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3(static_cast<unsigned>(rows * cs)); lc.blockDim = dim3(kCatThreads); lc.stream = ctx->stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = static_cast<unsigned>(cs); at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  lc.attrs = at; lc.numAttrs = 2;
+  CSD_CUDA(ctx, cudaLaunchKernelEx(&lc, kern, p));
+  ctx->launches++;
+  return CSD_OK;
+}
+
+int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_cat_params* f, const float* u, int32_t* token, float* logp, double* dist) {
+  CatParams p{};
+  p.R = static_cast<int>(R); p.V = V; p.logits = cat_view(l);
+  if (f) { p.temperature = f->temperature; p.top_k = f->top_k; p.top_p = f->top_p; p.min_p = f->min_p; }
+  p.u = u; p.token = token; p.logp = logp; p.dist = dist;
+  auto kern = l->dtype == CSD_F32 ? cat_filter_kernel<float> : l->dtype == CSD_BF16 ? cat_filter_kernel<__nv_bfloat16> : cat_filter_kernel<__half>;
+  return launch_cat(ctx, kern, R, cat_cluster(ctx, R, V), p);
+}
+
+int check_quant(csd_ctx* ctx, const uint8_t* data, const uint8_t* scale, const char* what) {
+  if (!data || !scale) return fail(ctx, CSD_ERR_INVALID_ARG, "%s matrix or its scales are null", what);
+  if (reinterpret_cast<uintptr_t>(data) % 16 || reinterpret_cast<uintptr_t>(scale) % 4) return fail(ctx, CSD_ERR_INVALID_ARG, "%s matrix must be 16-byte and its scales 4-byte aligned", what);
+  return CSD_OK;
+}
+
+template <typename T, bool NORM>
+int launch_quant_rows(csd_ctx* ctx, int rows, const QuantRowsParams& p) {
+  // pieces of eight columns a thread: one up to 4096 columns, then two and four; wider rows are read twice
+  const int pieces = p.ld / 8, nch = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 4096 ? 4 : 0;
+  const int threads = nch ? ((pieces + nch - 1) / nch + 31) / 32 * 32 : 1024;
+  auto kern = nch == 1 ? quant_rows_kernel<T, 1, NORM> : nch == 2 ? quant_rows_kernel<T, 2, NORM> : nch == 4 ? quant_rows_kernel<T, 4, NORM> : quant_rows_kernel<T, 0, NORM>;
+  return launch_short(ctx, ctx->stream, kern, rows, threads, 0, p);
+}
+
+template <bool NORM>
+int quant_rows(csd_ctx* ctx, int rows, int K, int dtype, QuantRowsParams p) {
+  if (rows < 1 || K < 1) return fail(ctx, CSD_ERR_INVALID_ARG, "rows = %d and K = %d must be >= 1", rows, K);
+  if (K > kQuantMaxK) return fail(ctx, CSD_ERR_UNSUPPORTED, "K = %d exceeds %d", K, kQuantMaxK);
+  if (dtype != CSD_F32 && dtype != CSD_BF16 && dtype != CSD_F16) return fail(ctx, CSD_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  const uintptr_t size = dtype == CSD_F32 ? 4 : 2;
+  if (!p.x) return fail(ctx, CSD_ERR_INVALID_ARG, "null array argument");
+  for (const void* a : {p.x, p.residual, p.weight, static_cast<const void*>(p.sum)})
+    if (reinterpret_cast<uintptr_t>(a) % size) return fail(ctx, CSD_ERR_INVALID_ARG, "an array is not aligned to its type");
+  if (p.ldx < 0 || p.ldr < 0 || (p.sum && rows > 1 && p.lds < K)) return fail(ctx, CSD_ERR_INVALID_ARG, "a row stride is negative, or the sum's rows overlap");
+  if (int rc = check_quant(ctx, p.data, p.scale, "the output")) return rc;
+  csd_quant_pitch(K, &p.ld, &p.ls);
+  p.K = K;
+  CSD_DEVICE(ctx);
+  return dtype == CSD_F32 ? launch_quant_rows<float, NORM>(ctx, rows, p) : dtype == CSD_BF16 ? launch_quant_rows<__nv_bfloat16, NORM>(ctx, rows, p)
+                                                                                             : launch_quant_rows<__half, NORM>(ctx, rows, p);
+}
+
+int make_quant_tmap(csd_ctx* ctx, CUtensorMap* m, const uint8_t* data, int rows, int ld, int box_rows) {
+  const cuuint64_t gdim[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t gstride[1] = {static_cast<cuuint64_t>(ld)};
+  const cuuint32_t box[2] = {kQuantBlock, static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUresult r = ctx->encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(data), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(ctx, CSD_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  return CSD_OK;
+}
+
+template <typename OUT>
+int launch_quant_mma(csd_ctx* ctx, const CUtensorMap& tw, const CUtensorMap& ta, const QuantMmaParams& p, int grid, size_t smem) {
+  auto kern = quant_mma_kernel<OUT>;
+  static bool attr_done[kMaxDevices] = {};   // function attributes are per device
+  if (!attr_done[ctx->device]) {
+    CSD_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+    attr_done[ctx->device] = true;
+  }
+  return launch_short(ctx, ctx->stream, kern, grid, kQmThreads, smem, tw, ta, p, ctx->d_err);
+}
+
 }  // namespace
 
 // ================================================================================== C ABI
@@ -2434,6 +2562,110 @@ int csd_gmm_resample(csd_ctx* ctx, int B, int gamma, int C, int cap, const csd_g
   auto kern = C <= 16 ? (fits ? gmm_resample_kernel<16, true> : gmm_resample_kernel<16, false>)
                       : (fits ? gmm_resample_kernel<32, true> : gmm_resample_kernel<32, false>);
   return launch_short(ctx, ctx->stream, kern, B, 128, fits ? smem : 0, r);
+}
+
+// ------------------------------------------------------------------ categorical heads
+int csd_cat_filter(csd_ctx* ctx, int R, int V, const csd_logits* logits, const csd_cat_params* params, double* dist) {
+  if (!ctx) return CSD_ERR_INVALID_ARG;
+  int rc = check_cat(ctx, logits, "the");
+  if (rc || (rc = check_cat_rows(ctx, R, V))) return rc;
+  if (!dist) return fail(ctx, CSD_ERR_INVALID_ARG, "null array argument");
+  CSD_DEVICE(ctx);
+  return cat_filter(ctx, R, V, logits, params, nullptr, nullptr, nullptr, dist);
+}
+
+int csd_cat_draft_sample(csd_ctx* ctx, int R, int V, const csd_logits* q, const csd_cat_params* params, const float* u, int32_t* token,
+                         float* logp, double* dist) {
+  if (!ctx) return CSD_ERR_INVALID_ARG;
+  int rc = check_cat(ctx, q, "draft");
+  if (rc || (rc = check_cat_rows(ctx, R, V))) return rc;
+  if (!u || !token) return fail(ctx, CSD_ERR_INVALID_ARG, "null array argument");
+  CSD_DEVICE(ctx);
+  return cat_filter(ctx, R, V, q, params, u, token, logp, dist);
+}
+
+int csd_cat_verify(csd_ctx* ctx, int B, int gamma, int rows_p, int V, const csd_logits* q, const double* dist_q, const csd_logits* p,
+                   const csd_cat_params* params_p, const int32_t* token, const float* u, double* dist_p, float* logratio,
+                   int32_t* n_accept, uint32_t* accept_mask) {
+  if (!ctx) return CSD_ERR_INVALID_ARG;
+  int rc = check_cat(ctx, q, "draft");
+  if (rc || (rc = check_cat(ctx, p, "target")) || (rc = check_cat_round(ctx, B, gamma, rows_p, V))) return rc;
+  if (!dist_q || !token || !u || !dist_p || !logratio || !n_accept) return fail(ctx, CSD_ERR_INVALID_ARG, "null array argument");
+  CSD_DEVICE(ctx);
+  if ((rc = cat_filter(ctx, static_cast<int64_t>(B) * rows_p, V, p, params_p, nullptr, nullptr, nullptr, dist_p))) return rc;
+  CatVerifyParams v{B, gamma, rows_p, V, cat_view(q), cat_view(p), dist_q, dist_p, token, u, logratio, n_accept, accept_mask};
+  return launch_short(ctx, ctx->stream, cat_verify_pick(q->dtype, p->dtype), (B + 3) / 4, 128, 0, v);
+}
+
+int csd_cat_resample(csd_ctx* ctx, int B, int gamma, int rows_p, int V, const csd_logits* q, const double* dist_q, const csd_logits* p,
+                     const double* dist_p, const int32_t* n_accept, const float* w, int32_t* x_new) {
+  if (!ctx) return CSD_ERR_INVALID_ARG;
+  int rc = check_cat(ctx, q, "draft");
+  if (rc || (rc = check_cat(ctx, p, "target")) || (rc = check_cat_round(ctx, B, gamma, rows_p, V))) return rc;
+  if (!dist_q || !dist_p || !n_accept || !w || !x_new) return fail(ctx, CSD_ERR_INVALID_ARG, "null array argument");
+  CSD_DEVICE(ctx);
+  CatResampleParams r{B, gamma, rows_p, V, cat_view(q), cat_view(p), dist_q, dist_p, n_accept, w, x_new};
+  return launch_cat(ctx, cat_resample_pick(q->dtype, p->dtype), B, cat_cluster(ctx, B, V), r);
+}
+
+// ------------------------------------------------------------------ 8-bit matrices
+int csd_quant_pitch(int K, int* ld, int* ls) {
+  if (K < 1 || !ld || !ls || K > kQuantMaxK) return CSD_ERR_INVALID_ARG;
+  const int blocks = (K + kQuantBlock - 1) / kQuantBlock;
+  *ld = blocks * kQuantBlock;
+  *ls = (blocks + 3) / 4 * 4;
+  return CSD_OK;
+}
+int csd_norm_quantize(csd_ctx* ctx, int rows, int K, int dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                      float eps, void* sum, int64_t lds, uint8_t* data, uint8_t* scale) {
+  if (!ctx) return CSD_ERR_INVALID_ARG;
+  if (!(eps >= 0.0f)) return fail(ctx, CSD_ERR_INVALID_ARG, "eps must be >= 0");
+  return quant_rows<true>(ctx, rows, K, dtype, QuantRowsParams{0, 0, 0, x, ldx, residual, ldr, weight, eps, sum, lds, data, scale});
+}
+
+int csd_quantize(csd_ctx* ctx, int rows, int K, int dtype, const void* x, int64_t ldx, uint8_t* data, uint8_t* scale) {
+  if (!ctx) return CSD_ERR_INVALID_ARG;
+  return quant_rows<false>(ctx, rows, K, dtype, QuantRowsParams{0, 0, 0, x, ldx, nullptr, 0, nullptr, 0.0f, nullptr, 0, data, scale});
+}
+
+int csd_quant_matmul(csd_ctx* ctx, int M, int N, int K, const csd_quant* a, const csd_quant* w, int dtype, void* out, int64_t ldo) {
+  if (!ctx) return CSD_ERR_INVALID_ARG;
+  if (M < 1 || N < 1 || K < 1) return fail(ctx, CSD_ERR_INVALID_ARG, "M = %d, N = %d, K = %d must be >= 1", M, N, K);
+  if (K > kQuantMaxK || M > (1 << 30) || N > (1 << 30)) return fail(ctx, CSD_ERR_UNSUPPORTED, "M = %d, N = %d or K = %d exceeds 2^30, 2^30 or %d", M, N, K, kQuantMaxK);
+  int rc = check_quant(ctx, a ? a->data : nullptr, a ? a->scale : nullptr, "the left");
+  if (rc || (rc = check_quant(ctx, w ? w->data : nullptr, w ? w->scale : nullptr, "the right"))) return rc;
+  if (dtype != CSD_F32 && dtype != CSD_BF16 && dtype != CSD_F16) return fail(ctx, CSD_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (!out || reinterpret_cast<uintptr_t>(out) % (dtype == CSD_F32 ? 4 : 2)) return fail(ctx, CSD_ERR_INVALID_ARG, "the output is null or not aligned to its type");
+  if (M > 1 && ldo < N) return fail(ctx, CSD_ERR_INVALID_ARG, "output rows of N = %d overlap at a stride of %lld", N, static_cast<long long>(ldo));
+  CSD_DEVICE(ctx);
+  int ld = 0, ls = 0;
+  csd_quant_pitch(K, &ld, &ls);
+  QuantMmaParams p{};
+  p.M = M; p.N = N; p.nkb = ld / kQuantBlock; p.ls = ls; p.scale_a = a->scale; p.scale_w = w->scale; p.out = out; p.ldo = ldo;
+  // token tiles as even as multiples of 32 allow
+  const int most = 224, mt = (M + most - 1) / most;
+  p.bn = ((M + mt - 1) / mt + 31) / 32 * 32;
+  p.tiles_m = (M + p.bn - 1) / p.bn;
+  const int64_t tiles = static_cast<int64_t>((N + 127) / 128) * p.tiles_m;
+  if (tiles > INT32_MAX) return fail(ctx, CSD_ERR_UNSUPPORTED, "too many output tiles");
+  p.tiles = static_cast<int>(tiles);
+  // few token rows leave room for two blocks an SM, whose loads and epilogues overlap
+  const int stage = kQmABytes + p.bn * kQuantBlock;
+  const bool two = p.bn <= 64;
+  const int room = two ? 113 * 1024 : 227 * 1024;
+  p.stages = (room - kQmFixed) / stage;
+  if (p.stages > 8) p.stages = 8;
+  p.acc_bufs = 2;
+  p.sf_col = p.acc_bufs * p.bn;
+  const int cols = p.sf_col + 2 * kQmSfCols;
+  for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
+  const int most_ctas = ctx->num_sms * (two ? 2 : 1);
+  const int grid = p.tiles < most_ctas ? p.tiles : most_ctas;
+  const size_t smem = kQmFixed + static_cast<size_t>(p.stages) * stage;
+  CUtensorMap tw, ta;
+  if ((rc = make_quant_tmap(ctx, &tw, w->data, N, ld, 128)) || (rc = make_quant_tmap(ctx, &ta, a->data, M, ld, p.bn))) return rc;
+  return dtype == CSD_F32 ? launch_quant_mma<float>(ctx, tw, ta, p, grid, smem) : dtype == CSD_BF16 ? launch_quant_mma<__nv_bfloat16>(ctx, tw, ta, p, grid, smem)
+                                                                                                 : launch_quant_mma<__half>(ctx, tw, ta, p, grid, smem);
 }
 
 int csd_round_host(csd_ctx* ctx, const csd_head* head_q, const csd_head* head_p, const csd_schedule* sched_q,

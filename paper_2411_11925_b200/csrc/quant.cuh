@@ -1,0 +1,363 @@
+// 8-bit matrices with a scale for each block of 128 columns, and what a vocabulary head does with them: the norm of the
+// backbone's output that leaves in 8 bits, and the product with the vocabulary matrix.
+//
+// An 8-bit matrix is [rows, ld] e4m3 with ld = K rounded up to 128 (padded with zeros) and [rows, ls] scales, one e8m0 byte a
+// block (2^(byte - 127), 255 = NaN), rows padded to a multiple of 4 with 127.  Scales are powers of two: e4m3 is a
+// floating format, so a finer scale would not make a value more exact, only keep 0.2 bit more of its range, and the tensor cores apply e8m0
+// scales inside the product (kind::mxf8f6f4), without a pass over the accumulators for each block.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "ptx.cuh"
+
+namespace csd {
+
+constexpr int kQuantBlock = 128;
+
+// ------------------------------------------------------------------------------------------------------------ the norm
+struct QuantRowsParams {
+  int K, ld, ls;
+  const void* x;
+  int64_t ldx;
+  const void* residual;   // null: none
+  int64_t ldr;
+  const void* weight;     // [K], null: ones
+  float eps;
+  void* sum;              // x + residual, null: not wanted; may be x or residual
+  int64_t lds;
+  uint8_t *data, *scale;
+};
+
+__device__ __forceinline__ float quant_to_float(float v) { return v; }
+__device__ __forceinline__ float quant_to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float quant_to_float(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T quant_from_float(float v);
+template <> __device__ __forceinline__ float quant_from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 quant_from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half quant_from_float<__half>(float v) { return __float2half_rn(v); }
+
+// Eight elements of a row from column `col` on, zeros behind the row's end; whole vectors where the row is 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void quant_load8(const T* row, int col, int K, bool aligned, float* v) {
+  if (aligned && col + 8 <= K) {
+    constexpr int kQ = sizeof(T) / 2;   // 16-byte vectors
+    __align__(16) T e[8];
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(e)[i] = reinterpret_cast<const uint4*>(row + col)[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = quant_to_float(e[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = col + i < K ? quant_to_float(row[col + i]) : 0.0f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void quant_store8(T* row, int col, int K, bool aligned, const float* v) {
+  if (aligned && col + 8 <= K) {
+    constexpr int kQ = sizeof(T) / 2;
+    __align__(16) T e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = quant_from_float<T>(v[i]);
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(row + col)[i] = reinterpret_cast<uint4*>(e)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (col + i < K) row[col + i] = quant_from_float<T>(v[i]);
+  }
+}
+
+// Eight values of a block whose largest magnitude has bits `amax`, to e4m3 under the block's scale byte: the smallest power
+// of two under which 448 = 1.75 2^8 reaches it (mantissas beyond 1.75 carry into the exponent).  A block with an infinity or a NaN is NaN.
+__device__ __forceinline__ uint32_t quant_scale_byte(uint32_t amax) {
+  if (amax >= 0x7f800000u) return 255u;
+  if (amax == 0u) return 127u;
+  const int b = static_cast<int>((amax + 0x1fffffu) >> 23) - 8;
+  return b > 0 ? static_cast<uint32_t>(b) : 0u;
+}
+__device__ __forceinline__ uint2 quant_pack8(const float* v, uint32_t byte) {
+  if (byte == 255u) return make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+  const float inv = __uint_as_float((254u - byte) << 23);   // 2^(127 - byte), exact
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(v[4 * i + 1] * inv), "f"(v[4 * i] * inv));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(v[4 * i + 3] * inv), "f"(v[4 * i + 2] * inv));
+    w[i] = static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// One block per row.  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read twice), 16 lanes a
+// scale block.  Sums and the norm in fp32; the sum leaves rounded to the input's type, the norm uses it unrounded.
+template <typename T, int NCH, bool NORM>
+__global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantRowsParams p) {
+  __shared__ float part[32];
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x, T_ = blockDim.x, pieces = p.ld / 8, lane = tid & 31;
+  griddep_enter();
+  const T* x = static_cast<const T*>(p.x) + r * p.ldx;
+  const T* res = p.residual ? static_cast<const T*>(p.residual) + r * p.ldr : nullptr;
+  const T* wt = static_cast<const T*>(p.weight);
+  T* sum = p.sum ? static_cast<T*>(p.sum) + r * p.lds : nullptr;
+  auto al = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
+  const bool ax = al(x), ar = al(res), aw = al(wt), as = al(sum);
+  uint8_t* data = p.data + r * p.ld;
+  uint8_t* scale = p.scale + r * p.ls;
+  auto load = [&](int c, float* h) {
+    quant_load8(x, c * 8, p.K, ax, h);
+    if (res) {
+      float v[8];
+      quant_load8(res, c * 8, p.K, ar, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] += v[i];
+    }
+  };
+  auto put = [&](int c, float* h, float rstd) {   // (whole groups of 16 lanes are inside or outside)
+    if (sum) quant_store8(sum, c * 8, p.K, as, h);
+    if (NORM) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] *= rstd;
+      if (wt) {
+        float v[8];
+        quant_load8(wt, c * 8, p.K, aw, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] *= v[i];
+      }
+    }
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(h[i]) & 0x7fffffffu);
+    const unsigned group = 0xffffu << (lane & 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(group, amax, o));
+    const uint32_t byte = quant_scale_byte(amax);
+    reinterpret_cast<uint2*>(data)[c] = quant_pack8(h, byte);
+    if ((lane & 15) == 0) scale[c >> 4] = static_cast<uint8_t>(byte);
+  };
+  for (int i = p.ld / kQuantBlock + tid; i < p.ls; i += T_) scale[i] = 127;
+  float rstd = 1.0f;
+  auto finish = [&](float ss) {
+    if (!NORM) return;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    if (lane == 0) part[tid >> 5] = ss;
+    __syncthreads();
+    ss = lane < (T_ >> 5) ? part[lane] : 0.0f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    rstd = rsqrtf(ss / static_cast<float>(p.K) + p.eps);
+  };
+  if (NCH > 0) {
+    float h[NCH > 0 ? NCH : 1][8], ss = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = tid + j * T_;
+      if (c < pieces) load(c, h[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      if (tid + j * T_ < pieces) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(h[j][i], h[j][i], ss);
+      }
+    }
+    finish(ss);
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+      if (tid + j * T_ < pieces) put(tid + j * T_, h[j], rstd);
+  } else {
+    float ss = 0.0f, h[8];
+    if (NORM)
+      for (int c = tid; c < pieces; c += T_) {
+        load(c, h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
+      }
+    finish(ss);
+    for (int c = tid; c < pieces; c += T_) { load(c, h); put(c, h, rstd); }
+  }
+}
+
+// --------------------------------------------------------------------------------------------------------- the product
+// out[m, n] = sum_k a[m, k] w[n, k], both 8-bit matrices.  The vocabulary matrix is the MMA's M operand (128 rows a
+// tile: N is never small), the token rows its N operand (a multiple of 32 up to 224, so that two accumulators and the scales
+// fit the 512 tensor-memory columns): a single token row costs what reading the weights costs.
+//   warp 0      requests both operands by TMA, a block of 128 columns a stage
+//   warp 1      issues the MMAs: four of K = 32 a stage under one scale byte (byte kb % 4 of the scale words)
+//   warps 2..5  bring the scales into tensor memory, a word (four blocks) per row: row 32 j + i at lane i, column j, in all
+//               four lane quarters
+//   warps 6..9  epilogue: a lane is a vocabulary row, a register a token
+struct QuantMmaParams {
+  int M, N, nkb, ls;          // token rows, vocabulary rows, blocks of 128 columns, scale bytes a row
+  int bn, stages, acc_bufs, sf_col, tmem_cols, tiles_m, tiles;
+  const uint8_t *scale_a, *scale_w;
+  void* out;
+  int64_t ldo;
+};
+constexpr int kQmThreads = 320;
+constexpr int kQmABytes = 128 * kQuantBlock;
+constexpr int kQmSfCols = 12;   // 4 of the weights' scales, up to 8 of the tokens'
+constexpr int kQmFixed = 1024 + 256;
+
+// (+)= with e8m0 scales from tensor memory; the scale byte is chosen by the instruction descriptor
+__device__ __forceinline__ void umma_mxf8(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+      ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(acc), "r"(sfa), "r"(sfb)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+
+template <typename OUT>
+__global__ void __launch_bounds__(kQmThreads, 2)
+quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, const QuantMmaParams p, int* err) {
+  extern __shared__ uint8_t qm_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(qm_raw) + 1023) & ~uintptr_t(1023));
+  const int stage_bytes = kQmABytes + p.bn * kQuantBlock, S = p.stages;
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + static_cast<size_t>(S) * stage_bytes);   // [8]
+  uint64_t* empty = full + 8;       // [8]
+  uint64_t* sf_full = empty + 8;    // [2]
+  uint64_t* sf_empty = sf_full + 2; // [2]
+  uint64_t* acc_full = sf_empty + 2;   // [2]
+  uint64_t* acc_empty = acc_full + 2;  // [2]
+  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int* s_abort = reinterpret_cast<int*>(tmem_s + 1);
+  if (threadIdx.x == 0) {
+    *s_abort = *reinterpret_cast<volatile int*>(err);
+    tma_prefetch_desc(&tm_w);
+    tma_prefetch_desc(&tm_a);
+    for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sf_full[i], 4); mbar_init(&sf_empty[i], 1); mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
+    fence_mbar_init();
+  }
+  __syncthreads();
+  if (*s_abort != 0) return;
+  if (warp == 1) { tmem_alloc(tmem_s, p.tmem_cols); tmem_relinquish(); }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_s;
+  griddep_wait();
+  if (threadIdx.x == 0) griddep_launch_dependents();
+  const int first = blockIdx.x, step = gridDim.x;
+  const int groups = (p.nkb + 3) / 4;
+  bool ok = true;
+  // a wait by a whole warp: one answer for all its lanes
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ch_wait<false>(bar, parity, err)) != 0; };
+  if (warp == 0) {
+    if (lane == 0) {
+      int it = 0;
+      for (int t = first; t < p.tiles && ok; t += step) {
+        const int n0 = t / p.tiles_m * 128, m0 = t % p.tiles_m * p.bn;
+        for (int kb = 0; kb < p.nkb; ++kb, ++it) {
+          const int s = it % S;
+          if (it >= S && !ch_wait<false>(&empty[s], ((it / S) & 1) ^ 1, err)) { ch_fail(err, 1, 9, it); ok = false; break; }
+          uint8_t* dst = ring + static_cast<size_t>(s) * stage_bytes;
+          mbar_arrive_expect_tx(&full[s], stage_bytes);
+          tma_load_2d(dst, &tm_w, &full[s], kb * kQuantBlock, n0);
+          tma_load_2d(dst + kQmABytes, &tm_a, &full[s], kb * kQuantBlock, m0);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    // e4m3 operands, K-major, fp32 accumulator, e8m0 scales, M = 128
+    const uint32_t idesc = (static_cast<uint32_t>(p.bn >> 3) << 17) | (1u << 23) | (8u << 24);
+    int it = 0, g = 0, i = 0;
+    for (int t = first; t < p.tiles && ok; t += step, ++i) {
+      const int ab = p.acc_bufs == 2 ? i & 1 : 0, use = p.acc_bufs == 2 ? i >> 1 : i;
+      if (use > 0 && !wait(&acc_empty[ab], (use - 1) & 1)) { if (leader) ch_fail(err, 2, 9, i); ok = false; break; }
+      tc_fence_after_sync();
+      const uint32_t d = tmem + ab * p.bn;
+      for (int kb = 0; kb < p.nkb; ++kb, ++it) {
+        const int s = it % S;
+        if ((kb & 3) == 0 && !wait(&sf_full[g & 1], (g >> 1) & 1)) { if (leader) ch_fail(err, 2, 10, g); ok = false; break; }
+        if (!wait(&full[s], (it / S) & 1)) { if (leader) ch_fail(err, 2, 11, it); ok = false; break; }
+        tc_fence_after_sync();
+        const bool last = (kb & 3) == 3 || kb == p.nkb - 1;
+        if (leader) {
+          const uint32_t base = smem_u32(ring + static_cast<size_t>(s) * stage_bytes);
+          const uint64_t da = umma_smem_desc_sw128(base), db = umma_smem_desc_sw128(base + kQmABytes);
+          const uint32_t id = idesc | (static_cast<uint32_t>(kb & 3) << 4) | (static_cast<uint32_t>(kb & 3) << 29);
+          const uint32_t sf = tmem + p.sf_col + (g & 1) * kQmSfCols;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) umma_mxf8(d, da + 2 * k, db + 2 * k, id, sf, sf + 4, kb > 0 || k > 0 ? 1u : 0u);
+          umma_commit(&empty[s]);
+          if (last) umma_commit(&sf_empty[g & 1]);
+        }
+        if (last) ++g;
+        __syncwarp();
+      }
+      if (ok && leader) umma_commit(&acc_full[ab]);
+      __syncwarp();
+    }
+  } else if (warp < 6) {
+    const int q = warp & 3, nb = p.bn / 32;
+    int g = 0;
+    for (int t = first; t < p.tiles && ok; t += step) {
+      const int n0 = t / p.tiles_m * 128, m0 = t % p.tiles_m * p.bn;
+      for (int j = 0; j < groups; ++j, ++g) {
+        uint32_t w[12];
+#pragma unroll
+        for (int i = 0; i < 12; ++i) {
+          w[i] = 0x7f7f7f7fu;
+          const int row = i < 4 ? n0 + 32 * i + lane : m0 + 32 * (i - 4) + lane;
+          if (i < 4 ? row < p.N : i - 4 < nb && row < p.M)
+            w[i] = __ldg(reinterpret_cast<const uint32_t*>((i < 4 ? p.scale_w : p.scale_a) + static_cast<int64_t>(row) * p.ls) + j);
+        }
+        if (g >= 2 && !wait(&sf_empty[g & 1], ((g >> 1) & 1) ^ 1)) { if (lane == 0) ch_fail(err, 2, 12, g); ok = false; break; }
+        tc_fence_after_sync();
+        const uint32_t at = tmem + p.sf_col + (g & 1) * kQmSfCols + (static_cast<uint32_t>(q * 32) << 16);
+        tmem_st4(at, w);
+        tmem_st4(at + 4, w + 4);
+        if (nb > 4) tmem_st4(at + 8, w + 8);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sf_full[g & 1]);
+      }
+    }
+  } else {
+    const int q = warp & 3;
+    int i = 0;
+    OUT* out = static_cast<OUT*>(p.out);
+    for (int t = first; t < p.tiles && ok; t += step, ++i) {
+      const int n = t / p.tiles_m * 128 + q * 32 + lane, m0 = t % p.tiles_m * p.bn;
+      const int ab = p.acc_bufs == 2 ? i & 1 : 0, use = p.acc_bufs == 2 ? i >> 1 : i;
+      if (!wait(&acc_full[ab], use & 1)) { if (lane == 0) ch_fail(err, 3, 9, i); ok = false; break; }
+      tc_fence_after_sync();
+      for (int c = 0; c < p.bn; c += 32) {
+        float v[32];
+        tmem_ld32(tmem + ab * p.bn + c + (static_cast<uint32_t>(q * 32) << 16), v);
+        tmem_ld_wait();
+        if (c + 32 >= p.bn) {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&acc_empty[ab]);
+        }
+        if (n < p.N) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (m0 + c + j < p.M) out[static_cast<int64_t>(m0 + c + j) * p.ldo + n] = quant_from_float<OUT>(v[j]);
+        }
+      }
+    }
+  }
+  if (!ok) settle();   // copies that nobody waits for any more
+  __syncthreads();
+  tc_fence_after_sync();
+  if (warp == 1) tmem_dealloc(tmem, p.tmem_cols);
+}
+
+}  // namespace csd

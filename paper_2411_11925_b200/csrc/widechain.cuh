@@ -251,7 +251,6 @@ struct WcParams {
   float ca[kWcMaxSteps], cb[kWcMaxSteps], s0[kWcMaxSteps], s1[kWcMaxSteps];   // index t - t_lo; s0: sigma, or LV the bounds s0, s1
 };
 
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"

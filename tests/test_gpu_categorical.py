@@ -1,0 +1,374 @@
+"""GPU parity of the categorical-head calls against plain 64-bit forms (tests/_cat.py).
+
+What may differ: a token whose border lies within the error of the weights' sums.  A weight is 2^-44 of the largest, rounded
+(2^-45), from an exponential with a relative error below 2^-42; over V tokens a prefix, relative to a sum of at least 1, is off by less than
+2^-41 + V 2^-45.  Log probabilities are differences of numbers of that error, returned in float32 (2^-24)."""
+import numpy as np
+import pytest
+import torch
+
+import _cat
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _ctx():
+    from paper_2411_11925_b200 import api
+    return api.Context(0)
+
+
+def _border(V):
+    return 2.0 ** -41 + V * 2.0 ** -45
+
+
+def _dev(a, t=None):
+    x = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return x if t is None else x.to(t)
+
+
+def _f32(x):
+    return x.float().cpu().numpy()
+
+
+def _sample(ctx, logits, u, params, R, V, dist=True):
+    tok = torch.full((R,), -7, dtype=torch.int32, device="cuda")
+    lp = torch.full((R,), 7.0, device="cuda")
+    d = torch.zeros(R, 5, dtype=torch.float64, device="cuda") if dist else None
+    ctx.csd_cat_draft_sample(R, V, logits, params, u, tok, lp, d)
+    ctx.sync()
+    return tok.cpu().numpy(), lp.cpu().numpy(), d.cpu().numpy() if dist else None
+
+
+def _check_rows(l32, tok, lp, d, u, fs):
+    V = l32.shape[1]
+    for r in range(l32.shape[0]):
+        order, logp, row = _cat.kept(l32[r], **fs[r])
+        assert d[r, 3] == row[3], (r, d[r], row, fs[r])
+        assert d[r, 1] == row[1] and d[r, 2] == row[2] and d[r, 4] == row[4], (r, d[r], row)
+        if order.size == 0:
+            assert tok[r] == -1 and lp[r] == -np.inf and d[r, 0] == -np.inf
+            continue
+        assert abs(d[r, 0] - row[0]) <= 2 * _border(V) + 4e-16 * (abs(row[0]) + abs(row[1])), (r, d[r], row)
+        w = np.zeros(V)
+        w[order] = np.exp(logp)
+        want, near = _cat.pick(w, u[r])
+        assert tok[r] == want or near < _border(V), (r, tok[r], want, near, fs[r])
+        got = logp[np.flatnonzero(order == tok[r])[0]]
+        assert abs(lp[r] - got) <= 2.0 ** -24 * abs(got) + 2 * _border(V) + 1e-15 * (abs(row[0]) + abs(row[1])), (r, lp[r], got)
+
+
+def _filters(rng, R, mixed):
+    one = lambda: dict(temperature=float(np.float32(rng.uniform(0.5, 1.5))), top_k=int(rng.choice([0, 1, 5, 50, 700])),  # noqa: E731
+                       top_p=float(np.float32(rng.choice([1.0, 0.3, 0.9, 0.999]))), min_p=float(np.float32(rng.choice([0.0, 0.0, 0.02, 1.0]))))
+    return [one() for _ in range(R)] if mixed else [dict() for _ in range(R)]
+
+
+def _params(fs):
+    if not fs[0]:
+        return None
+    col = lambda k, t: torch.tensor([f.get(k, {"temperature": 1.0, "top_k": 0, "top_p": 1.0, "min_p": 0.0}[k]) for f in fs], dtype=t, device="cuda")  # noqa: E731
+    return (col("temperature", torch.float32), col("top_k", torch.int32), col("top_p", torch.float32), col("min_p", torch.float32))
+
+
+@pytest.mark.parametrize("R,V,dtype,mixed", [(1, 1, "f32", False), (3, 2, "f32", True), (6, 7, "bf16", True), (5, 127, "f16", True),
+                                             (40, 1000, "f32", True), (7, 1000, "f32", False), (300, 4099, "bf16", True), (1, 16384, "f32", True),
+                                             (37, 50003, "bf16", True), (2, 131072, "f16", False), (2, 131072, "f32", True), (1, 300001, "f32", True)])
+def test_samples_match_the_plain_form(R, V, dtype, mixed):
+    rng = np.random.default_rng(V + R)
+    x = rng.standard_normal((R, V)) * 2.0
+    x[:, rng.integers(0, V, 5)] += rng.uniform(0, 9, 5)
+    x[rng.random((R, V)) < 0.1] = -np.inf
+    x[rng.random((R, V)) < 0.01] = np.nan
+    u = rng.random(R).astype(np.float32).clip(1e-7, 1 - 1e-7)
+    fs = _filters(rng, R, mixed)
+    ctx = _ctx()
+    l = _dev(x.astype(np.float32), TYPES[dtype])
+    tok, lp, d = _sample(ctx, l, _dev(u), _params(fs), R, V)
+    _check_rows(_f32(l), tok, lp, d, u, fs)
+    # the summaries alone are the same ones
+    d2 = torch.zeros(R, 5, dtype=torch.float64, device="cuda")
+    ctx.csd_cat_filter(R, V, l, _params(fs), d2)
+    ctx.sync()
+    np.testing.assert_array_equal(d2.cpu().numpy(), d)
+    ctx.close()
+
+
+@pytest.mark.parametrize("V,k,p", [(131072, 0, 0.95), (131072, 20000, 0.9), (60001, 5000, 1.0), (60001, 3000, 0.5), (9000, 0, 0.999), (131072, 0, 1.0)])
+def test_wide_filters(V, k, p):
+    """More tokens kept than a block sorts: flat rows, and rows of equals where only the index decides."""
+    rng = np.random.default_rng(k + V)
+    x = np.stack([rng.standard_normal(V), 1.5 * rng.standard_normal(V), np.zeros(V), np.round(2 * rng.standard_normal(V)), 1e-3 * rng.standard_normal(V),
+                  1e6 + rng.standard_normal(V)]).astype(np.float32)
+    u = rng.random(6).astype(np.float32)
+    fs = [dict(temperature=1.0, top_k=k, top_p=float(np.float32(p)), min_p=mp) for mp in (0.0, float(np.float32(0.01)), 0.0, 0.0, 0.0, 0.0)]
+    ctx = _ctx()
+    tok, lp, d = _sample(ctx, _dev(x), _dev(u), _params(fs), 6, V)
+    for r in range(6):
+        order, logp, row = _cat.kept(x[r], **fs[r])
+        if r != 2:   # (in a row of equals every border is a multiple of 1 / V: the count may be one off where p V is whole)
+            assert d[r, 3] == row[3], (r, d[r], row)
+    _check_rows(x[[0, 1, 3, 4, 5]], tok[[0, 1, 3, 4, 5]], lp[[0, 1, 3, 4, 5]], d[[0, 1, 3, 4, 5]], u[[0, 1, 3, 4, 5]], [fs[i] for i in (0, 1, 3, 4, 5)])
+    n = _cat.kept(x[2], **fs[2])[2][3]
+    assert abs(d[2, 3] - n) <= 1 and d[2, 2] == d[2, 3] - 1 and d[2, 1] == 0.0   # the first of the equals
+    assert 0 <= tok[2] < d[2, 3]
+    ctx.close()
+
+
+def test_rows_that_decide_by_rules():
+    """Masks and extremes: nothing left, one left, the type's lowest value, infinities, zero temperature, filters at their ends."""
+    V = 600
+    low = np.finfo(np.float32).min
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((16, V)).astype(np.float32)
+    x[0] = -np.inf
+    x[1] = np.nan
+    x[2] = -np.inf; x[2, 417] = -50.0
+    x[3] = low                                   # every token equally hopeless: uniform
+    x[4] = low; x[4, 99] = 3.0
+    x[5, 7] = np.inf                             # as the largest finite number
+    x[6, 3] = x[6, 400] = 99.0                   # equals at the top, zero temperature: the first
+    x[7, 5] = x[7, 450] = 50.0                   # top_k 1 among equals
+    x[8] = -np.inf; x[8, [3, 90, 200]] = [0.0, -0.0, 0.0]   # zeros of both signs are equals
+    x[9, ::2] = -np.inf                          # top_k beyond what is left
+    x[13] = 1e38; x[13, 50] = 3e38               # scaled beyond the range
+    fs = [dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) for _ in range(16)]
+    fs[3].update(temperature=0.5, top_p=0.5)
+    fs[4].update(temperature=0.25)
+    fs[6].update(temperature=0.0)
+    fs[7].update(top_k=1)
+    fs[8].update(top_k=2)
+    fs[9].update(top_k=500)
+    fs[10].update(top_p=0.0)
+    fs[11].update(top_p=-1.0, top_k=3)
+    fs[12].update(min_p=1.0)
+    fs[13].update(temperature=0.1)
+    fs[14].update(min_p=5.0)
+    fs[15].update(top_k=-4, top_p=1.5, min_p=-1.0)
+    u = np.full(16, 0.75, np.float32)
+    ctx = _ctx()
+    tok, lp, d = _sample(ctx, _dev(x), _dev(u), _params(fs), 16, V)
+    _check_rows(x, tok, lp, d, u, fs)
+    assert tok[0] == -1 and tok[1] == -1 and tok[2] == 417 and tok[4] == 99 and tok[5] == 7 and tok[6] == 3 and tok[7] == 5
+    assert tok[8] == 90 and d[8, 3] == 2 and d[8, 2] == 90
+    assert d[3, 3] == V // 2 and d[10, 3] == 1 and d[11, 3] == 1
+    # the ends of the uniform
+    for v in (1e-30, np.float32(1 - 2.0 ** -24), 0.0, 1.0):
+        tok, lp, d = _sample(ctx, _dev(x), _dev(np.full(16, v, np.float32)), _params(fs), 16, V)
+        assert np.all(tok[2:] >= 0) and np.all(np.isfinite(lp[2:]))
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_row_strides_and_alignments(dtype):
+    """Rows in a wider matrix, at every offset from a 16-byte border, behind one another with a gap, and one row for all."""
+    rng = np.random.default_rng(9)
+    ctx = _ctx()
+    wide = _dev(rng.standard_normal((5, 3011)).astype(np.float32) * 3, TYPES[dtype])
+    u = rng.random(5).astype(np.float32)
+    fs = _filters(rng, 5, True)
+    for off in range(0, 9):
+        for V in (1, 5, 1999):
+            l = wide[:, off:off + V]
+            tok, lp, d = _sample(ctx, l, _dev(u), _params(fs), 5, V)
+            _check_rows(_f32(l), tok, lp, d, u, fs)
+    same = wide[2:3, 11:2000].expand(5, -1)
+    tok, lp, d = _sample(ctx, same, _dev(u), _params(fs), 5, 1989)
+    _check_rows(_f32(same), tok, lp, d, u, fs)
+    ctx.close()
+
+
+def test_results_do_not_depend_on_how_a_row_is_spread():
+    """One row alone (several blocks) and the same row in a large batch (one block) give the same bits."""
+    rng = np.random.default_rng(21)
+    V = 33001
+    x = (rng.standard_normal((1, V)) * 1.5).astype(np.float32)
+    u = np.array([0.613], np.float32)
+    ctx = _ctx()
+    for k, p in ((0, 1.0), (0, 0.9), (40, 1.0), (4000, 0.8)):
+        f = dict(temperature=0.9, top_k=k, top_p=p, min_p=0.0)
+        one = _sample(ctx, _dev(x), _dev(u), _params([f]), 1, V)
+        for R in (60, 400):
+            many = _sample(ctx, _dev(x).expand(R, -1), _dev(np.repeat(u, R)), _params([f] * R), R, V)
+            for a, b in zip(one, many):
+                assert np.all(b == a[0]), (k, p, R)
+    ctx.close()
+
+
+def _round(ctx, x_q, x_p, fq, fp, u0, u, w, B, gamma, rows, V):
+    R = B * gamma
+    tok = torch.zeros(B, gamma, dtype=torch.int32, device="cuda")
+    dq = torch.zeros(R, 5, dtype=torch.float64, device="cuda"); dp = torch.zeros(B * rows, 5, dtype=torch.float64, device="cuda")
+    lr = torch.zeros(B, gamma, device="cuda")
+    n, mask, new = (torch.full((B,), 9, dtype=torch.int32, device="cuda") for _ in range(3))
+    ctx.csd_cat_draft_sample(R, V, x_q, fq, u0, tok, None, dq)
+    ctx.csd_cat_verify(B, gamma, rows, V, x_q, dq, x_p, fp, tok, u, dp, lr, n, mask)
+    ctx.csd_cat_resample(B, gamma, rows, V, x_q, dq, x_p, dp, n, w, new)
+    return tok, dq, dp, lr, n, mask, new
+
+
+@pytest.mark.parametrize("B,gamma,bonus,V,tq,tp,close", [(1, 1, True, 3, "f32", "f32", 0.5), (9, 5, True, 1000, "bf16", "f32", 0.3),
+                                                         (4, 32, False, 5003, "f16", "bf16", 0.2), (33, 4, True, 777, "f32", "f16", 1.0),
+                                                         (170, 2, True, 20011, "bf16", "bf16", 0.4), (2, 3, False, 131072, "f32", "f32", 0.1)])
+def test_round_matches_the_plain_form(B, gamma, bonus, V, tq, tp, close):
+    rng = np.random.default_rng(V + B)
+    rows = gamma + int(bonus)
+    p = rng.standard_normal((B, rows, V)) * 2
+    q = p[:, :gamma] + close * rng.standard_normal((B, gamma, V))
+    p[rng.random(p.shape) < 0.05] = -np.inf
+    x_q, x_p = _dev(q.reshape(-1, V).astype(np.float32), TYPES[tq]), _dev(p.reshape(-1, V).astype(np.float32), TYPES[tp])
+    fq, fp = _filters(rng, B * gamma, True), _filters(rng, B * rows, True)
+    u0, u, w = (rng.random(s).astype(np.float32).clip(1e-6, 1 - 1e-6) for s in (B * gamma, (B, gamma), B))
+    ctx = _ctx()
+    tok, dq, dp, lr, n, mask, new = [t.cpu().numpy() for t in _round(ctx, x_q, x_p, _params(fq), _params(fp), _dev(u0), _dev(u), _dev(w), B, gamma, rows, V)]
+    ctx.sync()
+    hq, hp = _f32(x_q), _f32(x_p).reshape(B, rows, V)
+    for b in range(B):
+        ok = []
+        for i in range(gamma):
+            pq, rq = _cat.probabilities(hq[b * gamma + i], **fq[b * gamma + i])
+            pp, rp = _cat.probabilities(hp[b, i], **fp[b * rows + i])
+            assert np.all(dq[b * gamma + i, 1:4] == rq[1:4]) and np.all(dp[b * rows + i, 1:4] == rp[1:4])
+            x = tok[b, i]
+            assert pq[x] > 0
+            with np.errstate(divide="ignore"):
+                want = np.log(pp[x]) - np.log(pq[x]) if pp[x] > 0 else -np.inf
+            if np.isinf(want):
+                assert lr[b, i] == want
+            else:
+                assert abs(lr[b, i] - want) <= 2.0 ** -24 * abs(want) + 4 * _border(V) + 1e-14 * 30
+            ok.append(np.log(np.float64(u[b, i])) <= want)
+        assert (int(mask[b]) & 0xFFFFFFFF) == sum(int(o) << i for i, o in enumerate(ok)), (b, ok)
+        assert n[b] == (ok + [False]).index(False)
+        j = int(n[b])
+        if j == rows:
+            assert new[b] == -1
+            continue
+        pp, _ = _cat.probabilities(hp[b, j], **fp[b * rows + j])
+        r = pp
+        if j < gamma:
+            pq, _ = _cat.probabilities(hq[b * gamma + j], **fq[b * gamma + j])
+            r = np.maximum(pp - pq, 0.0)
+            r = r if r.sum() > 0 else pp
+        want, near = _cat.pick(r, w[b])
+        # probabilities to 2^-42, rounded to 2^-53: relative to what is left of p
+        assert new[b] == want or near < (2.0 ** -41 + V * 2.0 ** -53) / r.sum(), (b, new[b], want, near)
+    ctx.close()
+
+
+def test_equal_models_accept_everything_and_rejections_without_residual_fall_back_to_p():
+    B, gamma, V = 5, 4, 3001
+    rng = np.random.default_rng(2)
+    p = (rng.standard_normal((B * (gamma + 1), V)) * 2).astype(np.float32)
+    x_p = _dev(p)
+    x_q = _dev(p.reshape(B, gamma + 1, V)[:, :gamma].reshape(-1, V))
+    u0, u, w = (rng.random(s).astype(np.float32) for s in (B * gamma, (B, gamma), B))
+    ctx = _ctx()
+    tok, dq, dp, lr, n, mask, new = _round(ctx, x_q, x_p, None, None, _dev(u0), _dev(u), _dev(w), B, gamma, gamma + 1, V)
+    ctx.sync()
+    assert torch.all(lr == 0) and torch.all(n == gamma) and torch.all(mask == 15)
+    for b in range(B):
+        pr, _ = _cat.probabilities(p.reshape(B, gamma + 1, V)[b, gamma])
+        assert new[b] == _cat.pick(pr, w[b])[0]
+    # a caller who rejects all the same: max(0, p - q) is nothing, the token is drawn from p
+    zero = torch.zeros_like(n)
+    ctx.csd_cat_resample(B, gamma, gamma + 1, V, x_q, dq, x_p, dp, zero, _dev(w), new)
+    ctx.sync()
+    for b in range(B):
+        pr, _ = _cat.probabilities(p.reshape(B, gamma + 1, V)[b, 0])
+        assert new[b] == _cat.pick(pr, w[b])[0]
+    # counts out of range, and tokens that are none, are answered and touch nothing else
+    n[:] = torch.tensor([-1, gamma + 1, 1 << 30, -(1 << 31), gamma], device="cuda", dtype=torch.int32)
+    ctx.csd_cat_resample(B, gamma, gamma + 1, V, x_q, dq, x_p, dp, n, _dev(w), new)
+    tok[0] = torch.tensor([-1, V, 1 << 30, -(1 << 31)], device="cuda", dtype=torch.int32)
+    ctx.csd_cat_verify(B, gamma, gamma + 1, V, x_q, dq, x_p, None, tok, _dev(u), dp, lr, n, mask)
+    ctx.sync()
+    assert new[:4].tolist() == [-1] * 4 and int(new[4]) >= 0
+    assert torch.all(lr[0] == -np.inf) and int(n[0]) == 0 and torch.all(n[1:] == gamma)
+    ctx.close()
+
+
+def test_masked_target_rows_reject_and_give_no_token():
+    B, gamma, V = 3, 2, 500
+    rng = np.random.default_rng(8)
+    p = rng.standard_normal((B, gamma, V)).astype(np.float32)
+    p[1] = -np.inf
+    q = rng.standard_normal((B * gamma, V)).astype(np.float32)
+    q[4] = np.nan                                    # a draft without a token
+    u = np.full((B, gamma), 1e-6, np.float32)
+    ctx = _ctx()
+    tok, dq, dp, lr, n, mask, new = _round(ctx, _dev(q), _dev(p.reshape(-1, V)), None, None, _dev(np.full(6, 0.5, np.float32)), _dev(u),
+                                           _dev(np.full(3, 0.5, np.float32)), B, gamma, gamma, V)
+    ctx.sync()
+    assert n.tolist() == [2, 0, 0] and new.tolist()[:2] == [-1, -1] and tok[2, 0] == -1 and lr[2, 0] == -np.inf
+    pr, _ = _cat.probabilities(p[2, 0])
+    assert int(new[2]) == _cat.pick(pr, 0.5)[0]      # nothing to take away from p
+    ctx.close()
+
+
+def test_bad_arguments_are_refused():
+    from paper_2411_11925_b200 import api
+    ctx = _ctx()
+    l = torch.zeros(2, 8, device="cuda"); u = torch.zeros(2, device="cuda"); t = torch.zeros(2, dtype=torch.int32, device="cuda")
+    d = torch.zeros(2, 5, dtype=torch.float64, device="cuda")
+    cases = [
+        (ValueError, lambda: ctx.csd_cat_filter(2, 9, l, None, d)),                     # rows of another length
+        (ValueError, lambda: ctx.csd_cat_filter(3, 8, l, None, d)),                     # too few rows
+        (ValueError, lambda: ctx.csd_cat_filter(2, 8, l.double(), None, d)),
+        (ValueError, lambda: ctx.csd_cat_filter(2, 8, l.cpu(), None, d)),
+        (ValueError, lambda: ctx.csd_cat_filter(2, 8, torch.zeros(8, 2, device="cuda").T, None, d)),
+        (ValueError, lambda: ctx.csd_cat_filter(2, 8, l, None, d[:1])),
+        (ValueError, lambda: ctx.csd_cat_filter(2, 8, l, None, d.float())),
+        (TypeError, lambda: ctx.csd_cat_filter(2, 8, l, (u, t, u), d)),
+        (ValueError, lambda: ctx.csd_cat_filter(2, 8, l, (u, u, u, u), d)),             # top_k is int32
+        (TypeError, lambda: ctx.csd_cat_filter(2, 8, None, None, d)),
+        (ValueError, lambda: ctx.csd_cat_draft_sample(2, 8, l, None, u[:1], t)),
+        (TypeError, lambda: ctx.csd_cat_draft_sample(2, 8, l, None, u, None)),
+        (-1, lambda: ctx.csd_cat_filter(0, 8, l, None, d)),
+        (-3, lambda: ctx.csd_cat_filter(1, (1 << 19) + 1, torch.zeros(1, (1 << 19) + 1, device="cuda"), None, d)),
+        (-2, lambda: ctx.csd_cat_verify(1, 1, 3, 8, l, d, torch.zeros(3, 8, device="cuda"), None, t, u, torch.zeros(3, 5, dtype=torch.float64, device="cuda"), u, t)),
+        (-3, lambda: ctx.csd_cat_verify(1, 33, 33, 8, torch.zeros(33, 8, device="cuda"), torch.zeros(33, 5, dtype=torch.float64, device="cuda"),
+                                        torch.zeros(33, 8, device="cuda"), None, torch.zeros(33, dtype=torch.int32, device="cuda"), torch.zeros(33, device="cuda"),
+                                        torch.zeros(33, 5, dtype=torch.float64, device="cuda"), torch.zeros(33, device="cuda"), t)),
+    ]
+    for want, call in cases:
+        if isinstance(want, int):
+            with pytest.raises(api.CsdError) as e:
+                call()
+            assert e.value.code == want
+        else:
+            with pytest.raises(want):
+                call()
+    ctx.sync()
+    ctx.close()
+
+
+def test_captured_calls_replay_on_new_inputs_and_other_streams():
+    B, gamma, V = 6, 3, 9001
+    rng = np.random.default_rng(31)
+    s = torch.cuda.Stream()
+    from paper_2411_11925_b200 import api
+    ctx, plain = api.Context(0, s), _ctx()
+    x_q, x_p = torch.zeros(B * gamma, V, device="cuda"), torch.zeros(B * (gamma + 1), V, device="cuda")
+    u0, u, w = (_dev(rng.random(n).astype(np.float32)) for n in (B * gamma, (B, gamma), B))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        _round(ctx, x_q, x_p, None, None, u0, u, w, B, gamma, gamma + 1, V)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            out = _round(ctx, x_q, x_p, None, None, u0, u, w, B, gamma, gamma + 1, V)
+    for k in range(3):
+        p = rng.standard_normal((B, gamma + 1, V)).astype(np.float32)
+        with torch.cuda.stream(s):
+            x_p.copy_(_dev(p.reshape(-1, V)))
+            x_q.copy_(_dev((p[:, :gamma] + 0.3 * rng.standard_normal((B, gamma, V))).reshape(-1, V).astype(np.float32)))
+            g.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in out]
+        want = _round(plain, x_q, x_p, None, None, u0, u, w, B, gamma, gamma + 1, V)
+        plain.sync()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), k
+    ctx.sync()
+    del g
+    ctx.close(); plain.close()
