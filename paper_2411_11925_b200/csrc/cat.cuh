@@ -8,38 +8,41 @@
 // reciprocal temperature.
 //
 // Weights are 64-bit fixed point (2^-44 of the row's largest), formed in fp64 from scaled logits rounded once to fp32:
-// integer sums do not depend on the order, so a cut or a token does not depend on how a row is spread over blocks, and the error of a
-// prefix sum stays below 2^-36: which of 10^5 tokens straddles top_p or u is decided as in 64-bit arithmetic.  (With fp32 weights one
-// flat row of 131072 tokens in a hundred had another count.)
+// integer sums do not depend on the order, so a cut or a token does not depend on how a row is spread over blocks, and a
+// prefix sum is off by 2^-42 of itself and 2^-45 a token: which of 10^5 tokens straddles top_p or u is decided as in 64-bit arithmetic.
 //
-// One cluster of 1 to 8 blocks carries a row; every pass reads the row again (DRAM the first time, L2 after): a pass from L2 costs
-// about what one from shared memory would, and V is not bounded by it.
+// Three kernels, each over (row, part of the row): the largest logit (cat_top_kernel); counts by distance from it, or what needs no
+// counts (cat_scan_kernel); weights and the few candidates for the cut (cat_range_kernel).  The last block of a row to arrive draws the
+// conclusion for the row.  One kernel that kept a row in a cluster took 2 to 4 times as long: its passes shared 64 registers with
+// everything a row's state needs, and a reduction through distributed shared memory cost 1.3 us.
 #pragma once
-#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <float.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include "ptx.cuh"
 
 namespace csd {
-namespace cg = cooperative_groups;
 typedef unsigned long long u64;
 
-constexpr int kCatThreads = 512;
+constexpr int kCatThreads = 256;
 constexpr int kCatWarps = kCatThreads / 32;
-constexpr int kCatBins = 2048;        // bins of the first histogram: 1/64 of scaled logit each, 32 below the largest
+constexpr int kCatBins = 2048;        // bins of the histogram: 1/64 of scaled logit each, 32 below the largest
 constexpr float kCatPerUnit = 64.0f;
+constexpr int kCatFrac = 12;          // bits of a token's place within its bin: the places of 2^19 tokens add up to less than 2^32
 constexpr int kCatList = 2048;        // candidates that are sorted
+constexpr int kCatRank = 512;         // candidates up to which they are sorted by counting
 constexpr int kCatSub = 1024;         // bins of a refinement
-constexpr int kCatSegs = 8;           // pieces of a warp's part whose sums are kept, of at least kCatUnroll rounds
-constexpr int kCatPairs = 256;        // kept tokens up to which a token is found by comparing all pairs
+constexpr int kCatPiece = 512;        // tokens whose weights are summed together, to find a token by its cumulative weight
 constexpr int kCatRow = 5;            // doubles of a row's summary
-constexpr int kCatMaxCluster = 8;
+constexpr int kCatTau = 256;          // top-k up to which its tokens are gathered by a threshold from the threads' maxima
+constexpr int kCatMaxV = 1 << 19;     // sums of 2^19 weights of 2^44 stay far below 2^64
+constexpr int kCatMaxPieces = kCatMaxV / kCatPiece + 1;   // (rows that do not start on 16 bytes)
 constexpr double kLog2e = 1.4426950408889634074;
-constexpr float kCatFar = 30.5f;      // further below the largest a weight is less than 2^-44: 0
+constexpr float kCatFloor = 32.0f;    // weights are 0 from here on down
 
 struct CatView {
   const void* data;
@@ -96,14 +99,15 @@ template <typename T> struct CatRow {
     head = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
     base = p - head;
   }
-  __device__ __forceinline__ int vecs() const { return (head + V + kVec - 1) / kVec; }
-  __device__ __forceinline__ uint4 load(int v) const {
+  __device__ __forceinline__ int pieces() const { return (head + V + kCatPiece - 1) / kCatPiece; }
+  __device__ __forceinline__ bool whole(int v) const { const int first = v * kVec - head; return first >= 0 && first + kVec <= V; }
+  __device__ __forceinline__ uint4 vec(int v) const { return __ldg(reinterpret_cast<const uint4*>(base) + v); }
+  __device__ __forceinline__ bool some(int v) const { return v * kVec - head < V; }
+  __device__ __forceinline__ static uint4 none() { const uint32_t mk = CatType<T>::masked(); return make_uint4(mk, mk, mk, mk); }
+  __device__ __noinline__ uint4 edge(int v) const {   // across an end of the row: masked outside
     const int first = v * kVec - head;
-    if (first >= 0 && first + kVec <= V) return __ldg(reinterpret_cast<const uint4*>(base) + v);
-    const uint32_t mk = CatType<T>::masked();
-    uint4 r = make_uint4(mk, mk, mk, mk);
     __align__(16) T e[kVec];
-    *reinterpret_cast<uint4*>(e) = r;
+    *reinterpret_cast<uint4*>(e) = none();
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
       if (first + i >= 0 && first + i < V) e[i] = base[static_cast<int64_t>(v) * kVec + i];
@@ -111,41 +115,64 @@ template <typename T> struct CatRow {
   }
 };
 
-constexpr int kCatUnroll = 4;
-// This warp's part of the row: `iters` rounds of 32 vectors, parts in index order over the warps of the cluster; `len` rounds a piece.
-struct CatPart {
-  int first, iters, len, vecs;
-  template <typename T> __device__ __forceinline__ CatPart(const CatRow<T>& r, int cs, int rank) : vecs(r.vecs()) {
-    const int warps = cs * kCatWarps;
-    iters = ((vecs + warps - 1) / warps + 31) / 32;
-    first = (rank * kCatWarps + (threadIdx.x >> 5)) * iters * 32;
-    len = max(kCatUnroll, (iters + kCatSegs - 1) / kCatSegs);
-  }
-};
+__device__ __forceinline__ u64 cat_warp_sum(u64 v) {   // in three pieces: 32 times 27 bits fit a word
+  const uint32_t a = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(v) & 0x7ffffffu);
+  const uint32_t b = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(v >> 27) & 0x7ffffffu);
+  const uint32_t c = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(v >> 54));
+  return a + (static_cast<u64>(b) << 27) + (static_cast<u64>(c) << 54);
+}
+__device__ __forceinline__ u64 cat_warp_max(u64 v) {
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(v >> 32));
+  const uint32_t lo = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(v >> 32) == hi ? static_cast<uint32_t>(v) : 0u);
+  return (static_cast<u64>(hi) << 32) | lo;
+}
 
-// f(scaled logits of a vector's elements, index of the first of them) for every vector of rounds [from, to); elements outside the row are masked.
-template <typename T, typename F>
-__device__ __forceinline__ void cat_each(const CatRow<T>& row, const CatPart& part, float inv_t, int from, int to, F f) {
-  constexpr int kVec = CatRow<T>::kVec;
-  const int lane = threadIdx.x & 31;
-  for (int it = from; it < to; it += kCatUnroll) {
-    uint4 raw[kCatUnroll];
+// f(logits, index of the first) for the vectors of pieces [p0, p1), a piece a warp; done(piece) after each.  Tokens outside the row are masked.
+template <typename T, typename F, typename D>
+__device__ __forceinline__ void cat_pieces(const CatRow<T>& row, int p0, int p1, F f, D done) {
+  constexpr int kVec = CatRow<T>::kVec, kIts = kCatPiece / (32 * kVec), kTwo = 4 / kIts;   // four vectors are requested at a time
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int p = p0 + warp; p < p1; p += kTwo * kCatWarps) {
+    uint4 raw[4];
+    bool all = true;
 #pragma unroll
-    for (int j = 0; j < kCatUnroll; ++j) {
-      const int v = part.first + (it + j) * 32 + lane;
-      if (it + j < to && v < part.vecs) raw[j] = row.load(v);
-      else { const uint32_t mk = CatType<T>::masked(); raw[j] = make_uint4(mk, mk, mk, mk); }
+    for (int j = 0; j < 4; ++j) {
+      const int q = p + j / kIts * kCatWarps, v = (q * kIts + j % kIts) * 32 + lane;
+      const bool in = q < p1 && row.whole(v);
+      all = all && in;
+      if (in) raw[j] = row.vec(v);
+    }
+    if (!all) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int q = p + j / kIts * kCatWarps, v = (q * kIts + j % kIts) * 32 + lane;
+        if (q >= p1 || !row.whole(v)) raw[j] = q < p1 && row.some(v) ? row.edge(v) : row.none();
+      }
     }
 #pragma unroll
-    for (int j = 0; j < kCatUnroll; ++j) {
-      if (it + j >= to) break;
-      float t[kVec];
-      CatType<T>::unpack(raw[j], t);
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) t[i] = cat_scale(t[i], inv_t);
-      f(t, (part.first + (it + j) * 32 + lane) * kVec - row.head);
+    for (int j = 0; j < 4; ++j) {
+      const int q = p + j / kIts * kCatWarps;
+      if (q >= p1) break;
+      float l[kVec];
+      CatType<T>::unpack(raw[j], l);
+      f(l, ((q * kIts + j % kIts) * 32 + lane) * kVec - row.head);
+      if (j % kIts == kIts - 1) done(q);
     }
   }
+}
+template <typename T, typename F>
+__device__ __forceinline__ void cat_each(const CatRow<T>& row, int p0, int p1, F f) { cat_pieces(row, p0, p1, f, [](int) {}); }
+// The same where f gives a vector's weight: the pieces' sums go to seg; returns this thread's own sum.
+template <typename T, typename F>
+__device__ __forceinline__ u64 cat_sums(const CatRow<T>& row, int p0, int p1, u64* seg, F f) {
+  u64 all = 0, sum = 0;
+  cat_pieces(row, p0, p1, [&](const float* l, int idx) { sum += f(l, idx); }, [&](int q) {
+    all += sum;
+    sum = cat_warp_sum(sum);
+    if ((threadIdx.x & 31) == 0) seg[q] = sum;
+    sum = 0;
+  });
+  return all;
 }
 
 // ------------------------------------------------------------------------------------------------------ arithmetic
@@ -181,17 +208,29 @@ __device__ __forceinline__ double cat_exp(float t, double c, const double* tab) 
 __device__ __forceinline__ void cat_table(double* tab) {
   if (threadIdx.x < 16) tab[threadIdx.x] = exp2(threadIdx.x / 16.0);
 }
-// Weight relative to the largest scaled logit m (c = -m log2(e)): 2^44 exp(t - m), rounded; at most a few units above 2^44.
-__device__ __forceinline__ u64 cat_weight(float t, float m, double c, const double* tab) {
-  if (!(m - t <= kCatFar)) return 0;
-  return static_cast<u64>(__double_as_longlong(cat_exp(t, c, tab) + 256.0) - __double_as_longlong(256.0));
-}
+// exp(t - norm) of scaled logits t as 2^((t - base) log2(e) + c).  Where norm is so large that fp64 would lose what t - norm is, base
+// is the nearest fp32 number: t - base is exact for every t that matters (within a factor of two of base).  What lies more
+// than `range` below (masked tokens, -inf and NaN, too) counts as `range`: its weight rounds to 0, and no argument leaves cat_exp's domain;
+// what lies above counts as norm itself, where no finite scaled logit lies.
+struct CatScale {
+  float base, floor, ceil;
+  double c;
+  __device__ __forceinline__ CatScale(double norm, float range) {
+    base = fabs(norm) >= 4096.0 ? static_cast<float>(norm) : 0.0f;
+    const double rest = norm - base;
+    c = -rest * kLog2e;
+    ceil = __double2float_ru(rest);
+    floor = ceil - range;
+  }
+  __device__ __forceinline__ double exp(float t, const double* tab) const { return cat_exp(fminf(fmaxf(t - base, floor), ceil), c, tab); }
+};
+// Weights are sums of doubles with 256 added to each: the bits of v + 256 are those of 256 plus v in units of 2^-44, so adding up
+// bits and taking off 256's as often gives the integer sum.
+constexpr u64 kCat256 = 0x4070000000000000ull;
+__device__ __forceinline__ u64 cat_bits(double v) { return static_cast<u64>(__double_as_longlong(v + 256.0)); }
+// Weight relative to the largest scaled logit: 2^44 exp(t - m), rounded; at most a few units above 2^44, 0 below 2^-45.
+__device__ __forceinline__ u64 cat_weight(float t, const CatScale& s, const double* tab) { return cat_bits(s.exp(t, tab)) - kCat256; }
 
-template <typename X> __device__ __forceinline__ X cat_warp_sum(X v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
 // Inclusive sum over the block's threads (exclusive = inclusive - v); part: kCatWarps values of shared memory.
 template <typename X> __device__ __forceinline__ X cat_block_scan(X v, X* part, X* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -207,25 +246,29 @@ template <typename X> __device__ __forceinline__ X cat_block_scan(X v, X* part, 
   return v + before;
 }
 
-// ---------------------------------------------------------------------------------------------------- shared memory
-struct CatShared {
-  uint32_t hist[kCatBins];
-  u64 list[kCatList];                       // candidates; a refinement's weights
-  u64 seg[kCatWarps * kCatSegs];            // sums of the pieces of the warps' parts
-  u64 red[2][kCatWarps][3];                 // reductions over the cluster, two in turn
-  u64 scan[kCatWarps];
-  double scan_d[kCatWarps];
-  double tab[16];
-  float maxima[kCatWarps];
-  // found by one thread, read by all (of the cluster: rank 0's)
-  u64 found_key, found_sum;
-  u64 found_count;
-  int found_a, found_b, found_n, found_seg;
-  uint32_t list_n;
+// ------------------------------------------------------------------------------------------------------- workspace
+struct CatTop { uint32_t top, tau, live, pad; };   // of a row's part: order of the largest logit and of the threshold, tokens not masked
+enum { CAT_DONE = 0, CAT_RANGE = 1, CAT_SEARCH = 2 };
+struct CatState {                                  // of a row
+  uint32_t ticket[2], list_n;
+  int mode;                                        // what is left to do for cat_range_kernel
+  uint32_t ua, ub, uk, ue;                         // places: list [ua, ub) and [uk, ue), weights below ua (and below uk)
+  uint32_t at_a, n1, n_mid;
+  int apart, upto, ends;
+};
+struct CatWork {
+  int rows, splits, share, pieces;                 // rows of this launch; parts of a row, pieces a part, pieces of the longest row
+  CatTop* top;                                     // [rows, splits]
+  CatState* state;                                 // [rows]
+  uint32_t* hist;                                  // [rows, 2, kCatBins]
+  u64* list;                                       // [rows, kCatList]
+  u64* seg;                                        // [rows, pieces]
+  u64* tot;                                        // [rows, splits, 3]
 };
 
 struct CatParams {
-  int R, V;
+  int V;
+  int64_t r0;                                      // first row of this launch
   CatView logits;
   const float* temperature;   // [R] or null: 1
   const int32_t* top_k;       // [R] or null
@@ -234,48 +277,104 @@ struct CatParams {
   int32_t* token;             // [R]
   float* logp;                // [R] or null
   double* dist;               // [R, 5] or null
+  CatWork w;
 };
 
-// Blocks of a row's cluster and the reductions between them.
-struct CatTeam {
-  cg::cluster_group cl;
-  int cs, rank, turn;
-  CatShared& sh;
-  __device__ __forceinline__ explicit CatTeam(CatShared& s) : cl(cg::this_cluster()), cs(cl.num_blocks()), rank(cl.block_rank()), turn(0), sh(s) {}
-  __device__ __forceinline__ void sync() { if (cs == 1) __syncthreads(); else cl.sync(); }
-  template <typename X> __device__ __forceinline__ X* at(X* p, int r) { return cs == 1 ? p : cl.map_shared_rank(p, r); }
-  // sums (a, b) and the maximum (c) over all threads of the cluster.  Slots are used in turn: a block is at most one
-  // reduction ahead of a block that still reads.
-  __device__ __forceinline__ void reduce(u64& a, u64& b, u64& c) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    a = cat_warp_sum(a); b = cat_warp_sum(b);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) { const u64 w = __shfl_xor_sync(0xffffffffu, c, o); c = w > c ? w : c; }
-    u64 (*slot)[3] = sh.red[turn];
-    turn ^= 1;
-    if (lane == 0) { slot[warp][0] = a; slot[warp][1] = b; slot[warp][2] = c; }
-    sync();
-    u64 x = 0, y = 0, z = 0;
-    for (int i = lane; i < cs * kCatWarps; i += 32) {
-      const u64* p = at(&slot[i % kCatWarps][0], i / kCatWarps);
-      x += p[0]; y += p[1]; z = p[2] > z ? p[2] : z;
-    }
-    a = cat_warp_sum(x); b = cat_warp_sum(y); c = z;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) { const u64 w = __shfl_xor_sync(0xffffffffu, c, o); c = w > c ? w : c; }
+// ---------------------------------------------------------------------------------------------------- shared memory
+struct CatShared {
+  __align__(16) uint32_t hist[2 * kCatBins];  // tokens per bin, sum of their places in it; later: sums of all pieces, words of a refinement
+  __align__(16) u64 list[kCatList];           // candidates
+  u64 scan[kCatWarps];
+  uint2 scan2[kCatWarps];
+  u64 red[kCatWarps][3];
+  double tab[16];
+  uint32_t rank[kCatRank];
+  CatTop top;
+  // found by one thread, read by all
+  u64 found_key, found_sum, found_upto, found_before[2];
+  uint32_t found_n;
+  int found_a, found_b, found_k, found_prev, found_listed, found_piece;
+  float found_lo, found_hi;
+  uint32_t at_a, at_b, at_k, end_k, list_n, base, last;
+  __device__ __forceinline__ void append(u64 key) {
+    const uint32_t i = atomicAdd(&list_n, 1u);
+    if (i < kCatList) list[i] = key;
   }
 };
+static_assert(2 * kCatBins * sizeof(uint32_t) >= kCatMaxPieces * sizeof(u64), "the pieces' sums fit the histogram's place");
+static_assert(2 * kCatBins >= 4 * kCatSub, "a refinement's words do too");
 
-// Sorts list[0, n) ascending (bitonic; padded to a power of two).  Steps within 64 neighbours stay in one warp.
-__device__ __forceinline__ void cat_sort(u64* list, int n) {
-  int P = 64;
+// Over the block's threads: the sums of a and b, the maximum of c.
+__device__ __forceinline__ void cat_reduce(CatShared& sh, u64& a, u64& b, u64& c) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  a = cat_warp_sum(a); b = cat_warp_sum(b); c = cat_warp_max(c);
+  __syncthreads();
+  if (lane == 0) { sh.red[warp][0] = a; sh.red[warp][1] = b; sh.red[warp][2] = c; }
+  __syncthreads();
+  a = 0; b = 0; c = 0;
+#pragma unroll
+  for (int i = 0; i < kCatWarps; ++i) { a += sh.red[i][0]; b += sh.red[i][1]; c = sh.red[i][2] > c ? sh.red[i][2] : c; }
+}
+
+// Inclusive sums of a count and a weight over the block's threads.
+__device__ __forceinline__ void cat_block_scan2(uint32_t& n, float& w, uint2* part, float* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, n, o);
+    const float y = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) { n += x; w += y; }
+  }
+  if (lane == 31) part[warp] = make_uint2(n, __float_as_uint(w));
+  __syncthreads();
+  uint32_t bn = 0;
+  float bw = 0.0f, all = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kCatWarps; ++i) {
+    const uint2 x = part[i];
+    if (i < warp) { bn += x.x; bw += __uint_as_float(x.y); }
+    all += __uint_as_float(x.y);
+  }
+  n += bn; w += bw;
+  *total = all;
+}
+
+// Sorts list[0, n) ascending.  Up to kCatRank entries: each counts those before it, the block's threads sharing an entry's
+// count (a bitonic network is a round through shared memory a step: 10 k cycles for 256 entries, where this takes 1.5 k).  More: bitonic,
+// padded to a power of two; steps within 64 neighbours stay in one warp.
+__device__ __forceinline__ void cat_sort(CatShared& sh, int n) {
+  u64* list = sh.list;
+  const int tid = threadIdx.x;
+  if (n <= kCatRank) {
+    int P = 32;
+    while (P < n && P < kCatThreads) P <<= 1;
+    const int groups = kCatThreads / P, share = (n + groups - 1) / groups, from = tid / P * share, to = min(from + share, n);
+    const int o0 = tid & (P - 1), o1 = o0 + kCatThreads;
+    for (int i = tid; i < n; i += kCatThreads) sh.rank[i] = 0;
+    const u64 k0 = o0 < n ? list[o0] : ~0ull, k1 = o1 < n ? list[o1] : ~0ull;
+    uint32_t b0 = 0, b1 = 0;
+    if (n <= kCatThreads) {
+      for (int j = from; j < to; ++j) b0 += list[j] < k0;
+    } else {
+      for (int j = from; j < to; ++j) { const u64 x = list[j]; b0 += x < k0; b1 += x < k1; }
+    }
+    __syncthreads();
+    if (o0 < n && b0) atomicAdd(&sh.rank[o0], b0);
+    if (o1 < n && b1) atomicAdd(&sh.rank[o1], b1);
+    __syncthreads();
+    if (tid < P && o0 < n) list[sh.rank[o0]] = k0;
+    if (o1 < n) list[sh.rank[o1]] = k1;
+    __syncthreads();
+    return;
+  }
+  int P = 1024;
   while (P < n) P <<= 1;
-  for (int i = n + static_cast<int>(threadIdx.x); i < P; i += kCatThreads) list[i] = ~0ull;
+  for (int i = n + tid; i < P; i += kCatThreads) list[i] = ~0ull;
   __syncthreads();
   for (int size = 2; size <= P; size <<= 1)
     for (int stride = size >> 1; stride > 0; stride >>= 1) {
-      for (int i = threadIdx.x; i < P / 2; i += kCatThreads) {
-        const int a = (i / stride) * 2 * stride + i % stride, b = a + stride;
+      for (int i = tid; i < P / 2; i += kCatThreads) {
+        const int a = ((i & ~(stride - 1)) << 1) | (i & (stride - 1)), b = a + stride;
         const u64 x = list[a], y = list[b];
         const bool up = (a & size) == 0;
         if ((x > y) == up) { list[a] = y; list[b] = x; }
@@ -285,72 +384,35 @@ __device__ __forceinline__ void cat_sort(u64* list, int n) {
   __syncthreads();
 }
 
-// ---------------------------------------------------------------------------------------------------- finding a token
-// The token at which the cumulative weight reaches target: sums of the pieces of all warps' parts are in every block's
-// sh.seg; the warp that owns the piece goes through it again.  weight(t, idx) as in the pass that formed the sums.
-template <typename T, typename W>
-__device__ __forceinline__ void cat_locate(CatTeam& team, const CatRow<T>& row, const CatPart& part, float inv_t, u64 target, W weight, int* token) {
-  CatShared& sh = team.sh;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int kVec = CatRow<T>::kVec;
-  team.sync();                                     // the pieces' sums are written
-  const int pieces = team.cs * kCatWarps * kCatSegs;   // at most 1024: two a thread
-  const int each = (pieces + kCatThreads - 1) / kCatThreads;
-  if (team.rank == 0) {
-    u64 s[2] = {0, 0};
-    for (int j = 0; j < each; ++j) {
-      const int i = threadIdx.x * each + j;
-      if (i < pieces) s[j] = *team.at(&sh.seg[i % (kCatWarps * kCatSegs)], i / (kCatWarps * kCatSegs));
-    }
-    u64 total;
-    u64 before = cat_block_scan<u64>(s[0] + s[1], sh.scan, &total) - s[0] - s[1];
-    for (int j = 0; j < each; ++j) {
-      if (before < target && before + s[j] >= target) { sh.found_seg = threadIdx.x * each + j; sh.found_sum = before; }
-      before += s[j];
-    }
-  }
-  team.sync();
-  const int piece = *team.at(&sh.found_seg, 0);
-  u64 before = *team.at(&sh.found_sum, 0);
-  if (piece / kCatSegs == team.rank * kCatWarps + warp) {
-    const int from = (piece % kCatSegs) * part.len, to = min(from + part.len, part.iters);
-    bool done = false;
-    for (int it = from; it < to && !done; ++it) {
-      cat_each(row, part, inv_t, it, it + 1, [&](const float* t, int idx) {
-        u64 w[kVec], s = 0;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) { w[i] = weight(t[i], idx + i); s += w[i]; }
-        u64 incl = s;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const u64 x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
-        u64 at = before + incl - s;
-        if (at < target && at + s >= target) {
-#pragma unroll
-          for (int i = 0; i < kVec; ++i) { if (at < target && at + w[i] >= target) *token = idx + i; at += w[i]; }
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
-        done = before >= target;
-      });
-    }
-  }
+// Whether this block is the last of its row's to come here; if so, what the others wrote before is visible to it.
+__device__ __forceinline__ bool cat_last(CatShared& sh, uint32_t* ticket, int splits) {
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) sh.last = splits == 1 || atomicAdd(ticket, 1u) == static_cast<uint32_t>(splits - 1);
+  __syncthreads();
+  if (!sh.last) return false;
+  __threadfence();
+  return true;
 }
-
-// One pass that leaves the sums of the warps' pieces in sh.seg; f(t, idx) gives an element's weight.
-template <typename T, typename F>
-__device__ __forceinline__ u64 cat_sums(CatTeam& team, const CatRow<T>& row, const CatPart& part, float inv_t, F f) {
-  constexpr int kVec = CatRow<T>::kVec;
-  u64 all = 0;
-  for (int s = 0; s < kCatSegs; ++s) {
-    u64 sum = 0;
-    cat_each(row, part, inv_t, s * part.len, min((s + 1) * part.len, part.iters), [&](const float* t, int idx) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) sum += f(t[i], idx + i);
-    });
-    all += sum;
-    sum = cat_warp_sum(sum);
-    if ((threadIdx.x & 31) == 0) team.sh.seg[(threadIdx.x >> 5) * kCatSegs + s] = sum;
-  }
-  return all;
+// This block's list goes to the row's in memory, ...
+__device__ __forceinline__ void cat_put_list(CatShared& sh, CatState* st, u64* list, int splits) {
+  __syncthreads();
+  const uint32_t n = sh.list_n;
+  if (splits == 1) return;
+  if (threadIdx.x == 0 && n > 0) sh.base = atomicAdd(&st->list_n, n);
+  __syncthreads();
+  if (n > 0 && n <= kCatList)
+    for (uint32_t i = threadIdx.x; i < n; i += kCatThreads)
+      if (sh.base + i < kCatList) __stcg(list + sh.base + i, sh.list[i]);
+}
+// ... and comes back whole to the last block: the number of entries (more than kCatList: not all of them).
+__device__ __forceinline__ int cat_get_list(CatShared& sh, const CatState* st, const u64* list, int splits) {
+  __syncthreads();
+  if (splits == 1) return static_cast<int>(min(sh.list_n, kCatList + 1u));
+  const uint32_t n = min(__ldcg(&st->list_n), kCatList + 1u);
+  for (uint32_t i = threadIdx.x; i < min(n, static_cast<uint32_t>(kCatList)); i += kCatThreads) sh.list[i] = __ldcg(list + i);
+  __syncthreads();
+  return static_cast<int>(n);
 }
 
 // The weight that top-p asks for (the likeliest token is kept whatever it asks).
@@ -361,339 +423,719 @@ __device__ __forceinline__ u64 cat_target(float u, u64 total) {
   return t > total ? total : t;
 }
 
+// The token at which the cumulative weight reaches target, by one block: seg has the sums of all pieces, without the weights of
+// the first `extra` entries of the list; the piece that holds the token is gone through again.  weight(l, idx): of a logit, as in
+// the pass that formed the sums, listed tokens included.  One lane gets the token.
+template <typename T, typename W, typename L>
+__device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, const u64* seg, u64 target, int extra, L listed, W weight) {
+  constexpr int kVec = CatRow<T>::kVec, kEach = (kCatMaxPieces + kCatThreads - 1) / kCatThreads;
+  const int tid = threadIdx.x, lane = tid & 31, pieces = row.pieces(), each = (pieces + kCatThreads - 1) / kCatThreads;
+  u64* all = reinterpret_cast<u64*>(sh.hist);
+  __syncthreads();
+  for (int i = tid; i < pieces; i += kCatThreads) all[i] = __ldcg(seg + i);
+  __syncthreads();
+  if (extra > 0) {
+    for (int i = tid; i < extra; i += kCatThreads) {
+      const u64 key = sh.list[i];
+      atomicAdd(&all[(static_cast<int>(static_cast<uint32_t>(key)) + row.head) / kCatPiece], listed(key));
+    }
+    __syncthreads();
+  }
+  u64 s = 0, total;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) if (j < each && tid * each + j < pieces) s += all[tid * each + j];
+  u64 before = cat_block_scan<u64>(s, sh.scan, &total) - s;
+  for (int j = 0; j < each; ++j) {
+    if (tid * each + j >= pieces) break;
+    const u64 x = all[tid * each + j];
+    if (before < target && before + x >= target) { sh.found_piece = tid * each + j; sh.found_sum = before; }
+    before += x;
+  }
+  __syncthreads();
+  int token = -1;
+  if (tid < 32) {   // (the piece's first and only warp)
+    const int piece = sh.found_piece;
+    before = sh.found_sum;
+    cat_each(row, piece, piece + 1, [&](const float* l, int idx) {
+      u64 w[kVec], s = 0;
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) { w[i] = weight(l[i], idx + i); s += w[i]; }
+      u64 incl = s;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const u64 x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
+      u64 at = before + incl - s;
+      if (at < target && at + s >= target) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) { if (at < target && at + w[i] >= target) token = idx + i; at += w[i]; }
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    });
+  }
+  return token;
+}
+
 // ----------------------------------------------------------------------------------------------------- refinement
-// The last element kept, where more elements than the list holds come into question: the first element in key order at which the
-// running count reaches `count` (BY_WEIGHT: the running weight reaches `limit`) among keys <= last.  [a, b] should hold it.
+// The last element kept, where more elements than the list holds come into question (many equals, rows of tiny spread), by one block: the first
+// element in key order at which the running count reaches `count` (BY_WEIGHT: the running weight reaches `limit`) among keys
+// <= last, searched in ever narrower intervals [a, b] of keys.  Weights of a bin are summed in three words of 15 bits
+// each: 2^17 tokens fit, so a bin that holds more adds up its carries (the words are folded whenever 2^17 tokens have been read).
 template <bool BY_WEIGHT, typename T>
-__device__ __forceinline__ u64 cat_refine(CatTeam& team, const CatRow<T>& row, const CatPart& part, float inv_t, float m, double c,
-                                          u64 a, u64 b, u64 last, u64 count, double limit) {
-  CatShared& sh = team.sh;
-  constexpr int kVec = CatRow<T>::kVec;
-  const int tid = threadIdx.x;
+__device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, float inv_t, const CatScale& sc, u64 last, u64 count, double limit) {
+  constexpr int kVec = CatRow<T>::kVec, kEach = kCatSub / kCatThreads, kFold = (1 << 17) / kCatPiece;
+  const int tid = threadIdx.x, pieces = row.pieces();
+  uint32_t* words = sh.hist + kCatSub;
+  u64 a = 0, b = last;
   for (;;) {
     const int top = 64 - __clzll(static_cast<long long>(b - a | 1));
     const int shift = top > 10 ? top - 10 : 0;
-    team.sync();                                   // nobody reads the arrays below any more
-    for (int i = tid; i < kCatSub; i += kCatThreads) { sh.hist[i] = 0; sh.list[i] = 0; }
-    if (tid == 0) sh.list_n = 0;
-    __syncthreads();
-    u64 n_before = 0, w_before = 0, none = 0;
-    cat_each(row, part, inv_t, 0, part.iters, [&](const float* t, int idx) {
+    u64 n_before = 0, w_before = 0, none = 0, n[kEach] = {}, w[kEach] = {};
+    for (int p0 = 0; p0 < pieces; p0 += kFold) {
+      __syncthreads();                               // nobody reads the arrays below any more
+      for (int i = tid; i < 4 * kCatSub; i += kCatThreads) sh.hist[i] = 0;
+      __syncthreads();
+      cat_each(row, p0, min(p0 + kFold, pieces), [&](const float* l, int idx) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const u64 key = cat_key(t[i], idx + i);
-        if (!(t[i] > -INFINITY) || key > b || key > last) continue;
-        const u64 w = BY_WEIGHT ? cat_weight(t[i], m, c, sh.tab) : 0;
-        if (key < a) { ++n_before; w_before += w; }
-        else {
-          const int s = static_cast<int>((key - a) >> shift);
-          atomicAdd(&sh.hist[s], 1u);
-          if (BY_WEIGHT) atomicAdd(&sh.list[s], w);
+        for (int i = 0; i < kVec; ++i) {
+          const float t = cat_scale(l[i], inv_t);
+          const u64 key = cat_key(t, idx + i);
+          if (!(t > -INFINITY) || key > b) continue;
+          const u64 x = BY_WEIGHT ? cat_weight(t, sc, sh.tab) : 0;
+          if (key < a) { ++n_before; w_before += x; }
+          else {
+            const int s = static_cast<int>((key - a) >> shift);
+            atomicAdd(&sh.hist[s], 1u);
+            if (BY_WEIGHT) {
+              atomicAdd(&words[s], static_cast<uint32_t>(x) & 0x7fffu);
+              atomicAdd(&words[kCatSub + s], static_cast<uint32_t>(x >> 15) & 0x7fffu);
+              atomicAdd(&words[2 * kCatSub + s], static_cast<uint32_t>(x >> 30));
+            }
+          }
         }
-      }
-    });
-    team.reduce(n_before, w_before, none);         // (also orders the histograms' additions before the reads below)
-    uint32_t n[2];
-    u64 w[2];
+      });
+      __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      n[j] = 0; w[j] = 0;
-      for (int r = 0; r < team.cs; ++r) {
-        n[j] += *team.at(&sh.hist[tid * 2 + j], r);
-        if (BY_WEIGHT) w[j] += *team.at(&sh.list[tid * 2 + j], r);
+      for (int j = 0; j < kEach; ++j) {
+        const int i = tid * kEach + j;
+        n[j] += sh.hist[i];
+        if (BY_WEIGHT) w[j] += words[i] + (static_cast<u64>(words[kCatSub + i]) << 15) + (static_cast<u64>(words[2 * kCatSub + i]) << 30);
       }
     }
-    u64 all_n, all_w = 0;
-    u64 pn = cat_block_scan<u64>(n[0] + n[1], sh.scan, &all_n) - n[0] - n[1] + n_before;
+    cat_reduce(sh, n_before, w_before, none);
+    u64 own_n = 0, own_w = 0, all_n, all_w = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) { own_n += n[j]; own_w += w[j]; }
+    u64 pn = cat_block_scan<u64>(own_n, sh.scan, &all_n) - own_n + n_before;
     u64 pw = w_before;
-    if (BY_WEIGHT) pw += cat_block_scan<u64>(w[0] + w[1], sh.scan, &all_w) - w[0] - w[1];
+    if (BY_WEIGHT) pw += cat_block_scan<u64>(own_w, sh.scan, &all_w) - own_w;
     auto reached = [&](u64 cn, u64 cw) { return BY_WEIGHT ? static_cast<double>(cw) >= limit : cn >= count; };
-    if (reached(n_before, w_before)) { b = a - 1; a = 0; continue; }        // not in [a, b]: before it
-    if (!reached(n_before + all_n, w_before + all_w)) {                     // behind it
-      if (b >= last) return last;
-      a = b + 1; b = last;
-      continue;
-    }
+    if (!reached(n_before + all_n, w_before + all_w)) return last;   // (all of them are kept)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (!reached(pn, pw) && reached(pn + n[j], pw + w[j])) { sh.found_a = tid * 2 + j; sh.found_n = static_cast<int>(n[j]); sh.found_count = pn; sh.found_sum = pw; }
+    for (int j = 0; j < kEach; ++j) {
+      if (!reached(pn, pw) && reached(pn + n[j], pw + w[j])) { sh.found_a = tid * kEach + j; sh.found_n = static_cast<uint32_t>(n[j]); sh.found_before[0] = pn; sh.found_before[1] = pw; }
       pn += n[j]; pw += w[j];
     }
+    if (tid == 0) sh.list_n = 0;
     __syncthreads();
     a += static_cast<u64>(sh.found_a) << shift;
     const u64 span = (1ull << shift) - 1;
     b = b - a > span ? a + span : b;
-    const int inside = sh.found_n;
-    pn = sh.found_count; pw = sh.found_sum;
+    const int inside = static_cast<int>(sh.found_n);
+    pn = sh.found_before[0]; pw = sh.found_before[1];
     if (inside > kCatList) continue;
-    // few enough: sorted by the first block
-    team.sync();
-    cat_each(row, part, inv_t, 0, part.iters, [&](const float* t, int idx) {
+    // few enough to be sorted
+    cat_each(row, 0, pieces, [&](const float* l, int idx) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        const u64 key = cat_key(t[i], idx + i);
-        if (t[i] > -INFINITY && key >= a && key <= b && key <= last) team.at(sh.list, 0)[atomicAdd(team.at(&sh.list_n, 0), 1u)] = key;
+        const float t = cat_scale(l[i], inv_t);
+        const u64 key = cat_key(t, idx + i);
+        if (t > -INFINITY && key >= a && key <= b) sh.append(key);
       }
     });
-    team.sync();
-    if (team.rank == 0) {
-      cat_sort(sh.list, inside);
-      if (!BY_WEIGHT) {
-        if (tid == 0) sh.found_key = sh.list[count - pn - 1];
-      } else {
-        constexpr int kEach = kCatList / kCatThreads;
-        u64 lw[kEach], s = 0;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int i = tid * kEach + j;
-          lw[j] = i < inside ? cat_weight(cat_key_value(sh.list[i]), m, c, sh.tab) : 0;
-          s += lw[j];
-        }
-        u64 total;
-        u64 before = cat_block_scan<u64>(s, sh.scan, &total) - s + pw;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int i = tid * kEach + j;
-          if (i < inside && !reached(0, before) && reached(0, before + lw[j])) sh.found_key = sh.list[i];
-          before += lw[j];
-        }
-      }
-    }
-    team.sync();
-    return *team.at(&sh.found_key, 0);
-  }
-}
-
-// ------------------------------------------------------------------------------------------- summary of a row, and a token
-__device__ __forceinline__ int cat_bin(float m, float t) {   // kCatBins and more: below every bin
-  const float x = fminf((m - t) * kCatPerUnit, 4095.0f);
-  return __float2int_rd(x);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kCatThreads, 2) cat_filter_kernel(const CatParams p) {
-  __shared__ CatShared sh;
-  CatTeam team(sh);
-  const int tid = threadIdx.x;
-  constexpr int kVec = CatRow<T>::kVec;
-  const int64_t r = blockIdx.x / team.cs;
-  griddep_enter();
-  const float temp = p.temperature ? p.temperature[r] : 1.0f;
-  const bool greedy = !(temp > 0.0f);
-  const float inv_t = greedy ? 1.0f : __fdiv_rn(1.0f, temp);
-  const int want = greedy ? 1 : (p.top_k ? p.top_k[r] : 0);
-  const u64 k = want > 0 && want < p.V ? static_cast<u64>(want) : static_cast<u64>(p.V);
-  const float tp = p.top_p ? p.top_p[r] : 1.0f, mp = p.min_p ? p.min_p[r] : 0.0f;
-  const bool by_k = k < static_cast<u64>(p.V), by_p = tp < 1.0f && !greedy;
-  const double min_d = mp > 0.0f ? log(static_cast<double>(fminf(mp, 1.0f))) : -INFINITY;   // kept: t - m >= min_d
-  const CatRow<T> row(p.logits, r, p.V);
-  const CatPart part(row, team.cs, team.rank);
-
-  // the largest scaled logit: scaling is monotonic, so it is the largest logit's
-  cat_table(sh.tab);
-  for (int i = tid; i < kCatBins; i += kCatThreads) sh.hist[i] = 0;
-  if (tid == 0) sh.list_n = 0;
-  float m = -INFINITY;
-  cat_each(row, part, inv_t, 0, part.iters, [&](const float* t, int) {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) m = fmaxf(m, t[i]);
-  });
-  {
-    u64 x = 0, y = 0, z = ~static_cast<u64>(cat_ord(m));   // ascending in m
-    team.reduce(x, y, z);
-    const u64 o = ~z;
-    m = cat_key_value(o << 32);
-  }
-  double* dist = p.dist ? p.dist + r * kCatRow : nullptr;
-  if (!(m > -INFINITY)) {   // nothing is left
-    if (team.rank == 0 && tid == 0) {
-      if (dist) { dist[0] = -INFINITY; dist[1] = INFINITY; dist[2] = -1.0; dist[3] = 0.0; dist[4] = inv_t; }
-      if (p.u) { p.token[r] = -1; if (p.logp) p.logp[r] = -INFINITY; }
-    }
-    team.sync();
-    return;
-  }
-  const double md = m, c = -md * kLog2e;
-  auto weight = [&](float t) { return cat_weight(t, m, c, sh.tab); };
-  auto likely = [&](float t) { return static_cast<double>(t) - md >= min_d; };
-
-  u64 cut = ~0ull;          // last key kept by top-k and top-p
-  bool listed = false;      // the kept tokens are the first of the first block's sorted list
-  u64 kept_n = 0, kept_w = 0, kept_last = 0;
-  if (by_k || by_p) {
-    // counts by distance from the largest, and the sum of all weights where top-p refers to it
-    const bool with_sum = by_p && k > kCatList / 2;
-    u64 live = 0, sum = 0, none = 0;
-    cat_each(row, part, inv_t, 0, part.iters, [&](const float* t, int) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        if (!(t[i] > -INFINITY)) continue;
-        ++live;
-        const int b = cat_bin(m, t[i]);
-        if (b < kCatBins) atomicAdd(&sh.hist[b], 1u);
-        if (with_sum) sum += weight(t[i]);
-      }
-    });
-    team.reduce(live, sum, none);
-    const bool k_counts = by_k && k < live;
-    const bool p_all = by_p && !k_counts && with_sum;   // top-p refers to the whole row, whose sum is known
-    // the bin where the count reaches k, or the bins between which the weight reaches top_p of the sum
-    uint32_t n[4] = {0, 0, 0, 0};
-    for (int q = 0; q < team.cs; ++q) {
-      const uint4 h = *reinterpret_cast<const uint4*>(team.at(&sh.hist[tid * 4], q));
-      n[0] += h.x; n[1] += h.y; n[2] += h.z; n[3] += h.w;
-    }
-    u64 binned;
-    u64 cum = cat_block_scan<u64>(static_cast<u64>(n[0]) + n[1] + n[2] + n[3], sh.scan, &binned) - n[0] - n[1] - n[2] - n[3];
-    double e[4], es = 0.0, et;
-    const double limit = cat_limit(tp, sum);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) { e[j] = n[j] * static_cast<double>(exp2f(-static_cast<float>(kLog2e) * (tid * 4 + j + 0.5f) / kCatPerUnit)); es += e[j]; }
-    double mass = cat_block_scan<double>(es, sh.scan_d, &et) - es;
-    if (tid == 0) { sh.found_a = kCatBins; sh.found_b = kCatBins; sh.found_n = 0; }
     __syncthreads();
-    // a bin's weight lies within exp(+-1/128) of its count times its middle's weight (and what rounding adds)
-    const double unit = 17592186044416.0;   // 2^44
-    const double lo = unit * 0.99221 * 0.99999, hi = unit * 1.00785 * 1.00001;
+    cat_sort(sh, inside);
+    if (!BY_WEIGHT) return sh.list[count - pn - 1];
+    constexpr int kMine = kCatList / kCatThreads;
+    u64 s = 0, total;
+    for (int j = 0; j < kMine; ++j) { const int i = tid * kMine + j; if (i < inside) s += cat_weight(cat_key_value(sh.list[i]), sc, sh.tab); }
+    u64 before = cat_block_scan<u64>(s, sh.scan, &total) - s + pw;
+    for (int j = 0; j < kMine; ++j) {
+      const int i = tid * kMine + j;
+      const u64 x = i < inside ? cat_weight(cat_key_value(sh.list[i]), sc, sh.tab) : 0;
+      if (i < inside && !reached(0, before) && reached(0, before + x)) sh.found_key = sh.list[i];
+      before += x;
+    }
+    __syncthreads();
+    return sh.found_key;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------ a row's settings
+// a threshold in the order of keys: kept are t > value, and t = value up to the index
+struct CatBound {
+  float value;
+  int idx;
+  __device__ __forceinline__ bool kept(float t, int i) const { return t > value || (t == value && i <= idx); }
+};
+// Distance from the largest in units of 1/64, kCatFrac bits behind the point; kCatBins and more: below every bin (masked too).
+__device__ __forceinline__ uint32_t cat_place(float m, float l, float inv_t) {
+  return __float2uint_rd(fminf((m - __fmul_rn(l, inv_t)) * (kCatPerUnit * (1 << kCatFrac)), 4095.0f * (1 << kCatFrac)));
+}
+struct CatRequest {   // what the caller asks of a row
+  float inv_t, top_p;
+  int want;           // top-k, 0: off
+  bool by_p, few;
+  __device__ __forceinline__ CatRequest(const CatParams& p, int64_t r) {
+    const float temp = p.temperature ? p.temperature[r] : 1.0f;
+    const bool greedy = !(temp > 0.0f);
+    inv_t = greedy ? 1.0f : __fdiv_rn(1.0f, temp);
+    want = greedy ? 1 : (p.top_k ? p.top_k[r] : 0);
+    if (want <= 0 || want >= p.V) want = 0;
+    top_p = p.top_p ? p.top_p[r] : 1.0f;
+    by_p = top_p < 1.0f && !greedy;
+    few = want > 0 && want <= kCatTau;
+  }
+};
+// The least scaled logit that min-p keeps: the smallest fp32 number not below m + log(min_p).
+__device__ __forceinline__ float cat_least(const CatParams& p, int64_t r, float m) {
+  const float mp = p.min_p ? p.min_p[r] : 0.0f;
+  if (!(mp > 0.0f)) return -INFINITY;
+  const double md = m, d = log(static_cast<double>(fminf(mp, 1.0f)));
+  float least = static_cast<float>(md + d);
+  while (static_cast<double>(least) - md < d) least = nextafterf(least, INFINITY);
+  while (static_cast<double>(nextafterf(least, -INFINITY)) - md >= d) least = nextafterf(least, -INFINITY);
+  return least;
+}
+// All parts' tops of a row, for every thread.
+__device__ __forceinline__ CatTop cat_tops(CatShared& sh, const CatWork& w, int row) {
+  if (threadIdx.x < 32) {
+    uint32_t a = 0xffffffffu, b = 0, n = 0;
+    for (int i = threadIdx.x; i < w.splits; i += 32) {
+      const CatTop t = w.top[static_cast<int64_t>(row) * w.splits + i];
+      a = min(a, t.top); b = max(b, t.tau); n += t.live;
+    }
+    a = __reduce_min_sync(0xffffffffu, a); b = __reduce_max_sync(0xffffffffu, b); n = __reduce_add_sync(0xffffffffu, n);
+    if (threadIdx.x == 0) sh.top = CatTop{a, b, n, 0};
+  }
+  __syncthreads();
+  return sh.top;
+}
+
+// ------------------------------------------------------------------------------------------------------- conclusions
+// What a row's cut is derived from: the list of n candidates; before the first of them n_above tokens of weight
+// w_above are kept for certain; between those of the first n1 (where top-p ends) and the rest (where top-k ends, if that is apart)
+// lie n_mid; w_upto is the weight of all tokens before the rest.
+struct CatCut {
+  int n, n1;
+  uint32_t n_above, n_mid;
+  u64 w_above, w_upto;
+  bool by_k, by_p, apart, ends;                    // ends: nothing behind the first n1 is kept (min-p)
+  uint32_t k;
+  float top_p, least;
+};
+struct CatKept {       // the conclusion
+  u64 last;            // key of the last token kept
+  u64 n, w;
+  int listed;          // so many of them are the first ones of the list, and not in the pieces' sums
+};
+// False: the list does not hold the cut.
+__device__ __noinline__ bool cat_resolve(CatShared& sh, const CatCut& x, const CatScale& sc, CatKept& out) {
+  const int tid = threadIdx.x;
+  constexpr int kEach = kCatList / kCatThreads;
+  cat_sort(sh, x.n);
+  // a thread holds `each` entries in a row
+  const int each = x.n <= kCatThreads ? 1 : x.n <= 2 * kCatThreads ? 2 : kEach;
+  // where top-k ends in the list
+  const int end_k = x.by_k ? static_cast<int>(x.k - x.n_above - x.n_mid) - 1 : x.n - 1;
+  u64 s = 0, total;
+  u64* lw = reinterpret_cast<u64*>(sh.hist);   // (the entries' weights; of this thread)
+  for (int j = 0; j < each; ++j) {
+    const int i = tid * each + j;
+    const u64 v = i < x.n ? cat_weight(cat_key_value(sh.list[i]), sc, sh.tab) : 0;
+    lw[i] = v;
+    s += v;
+  }
+  const u64 start = cat_block_scan<u64>(s, sh.scan, &total) - s;
+  if (tid == 0) { sh.found_upto = 0; sh.found_sum = total; sh.found_listed = 0; }
+  __syncthreads();
+  u64 before = start;
+  for (int j = 0; j < each; ++j) {
+    const int i = tid * each + j;
+    before += lw[i];
+    if (i == end_k) sh.found_sum = before;
+    if (i == x.n1 - 1) sh.found_upto = before;
+  }
+  __syncthreads();
+  double limit = INFINITY;
+  if (x.by_p) limit = cat_limit(x.top_p, !x.by_k ? x.w_upto : x.apart ? x.w_upto + sh.found_sum - sh.found_upto : x.w_above + sh.found_sum);
+  const int most = min(end_k, x.n1 - 1);
+  before = start + x.w_above;
+  int mine = 0;
+  for (int j = 0; j < each; ++j) {
+    const int i = tid * each + j;
+    mine += i <= most && ((i == 0 && x.n_above == 0) || (static_cast<double>(before) < limit && cat_key_value(sh.list[i]) >= x.least));
+    before += lw[i];
+  }
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  __syncthreads();                             // found_sum has been read
+  if ((tid & 31) == 0) sh.rank[tid >> 5] = mine;
+  __syncthreads();
+  int all = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int b = tid * 4 + j;
-      if (k_counts) {
-        if (cum < k && cum + n[j] >= k) { sh.found_a = b; sh.found_b = b; sh.found_n = static_cast<int>(min(cum + n[j], static_cast<u64>(INT_MAX))); }
-      } else if (p_all) {
-        if (mass * hi < limit && (mass + e[j]) * hi >= limit) sh.found_a = b;
-        if (mass * lo < limit && (mass + e[j]) * lo >= limit) { sh.found_b = b; sh.found_n = static_cast<int>(min(cum + n[j], static_cast<u64>(INT_MAX))); }
+  for (int i = 0; i < kCatWarps; ++i) all += sh.rank[i];
+  const int last = all - 1;
+  before = start + x.w_above;
+  for (int j = 0; j < each; ++j) {
+    const int i = tid * each + j;
+    before += lw[i];
+    // the cut is certain if the next one in the list is not kept, if top-k ends here, or if top-p's weight is reached here
+    if (i == last && (last < most || last == end_k || x.ends || static_cast<double>(before) >= limit)) { sh.found_listed = all; sh.found_sum = before; }
+  }
+  __syncthreads();
+  if (sh.found_listed == 0) return false;
+  out.last = sh.list[last]; out.n = x.n_above + static_cast<u64>(all); out.w = sh.found_sum; out.listed = all;
+  __syncthreads();
+  return true;
+}
+
+// One pass over pieces: weights of the tokens that `bound` keeps, their sums by piece; for this thread their weight, number and last key.
+template <typename T>
+__device__ __forceinline__ u64 cat_keep(const CatRow<T>& row, int p0, int p1, u64* seg, float inv_t, const CatScale& sc, const double* tab, CatBound bound, u64& n, u64& last) {
+  constexpr int kVec = CatRow<T>::kVec;
+  float end_t = INFINITY;   // the last token kept: the least, the highest index of its equals
+  int end_i = 0;
+  uint32_t count = 0;
+  const u64 w = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+    u64 sum = 0;
+#pragma unroll
+    for (int h = 0; h < kVec; h += 4) {     // four exponentials side by side
+      float t[4];
+      bool any = false, in[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        t[i] = cat_scale(l[h + i], inv_t);
+        in[i] = bound.kept(t[i], idx + h + i);
+        any = any || in[i];
+        if (in[i] && t[i] <= end_t) { end_t = t[i]; end_i = idx + h + i; }   // (a thread's indexes ascend)
+        count += in[i];
+      }
+      if (!__any_sync(0xffffffffu, any)) continue;
+      double x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = sc.exp(t[i], tab);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += cat_bits(in[i] ? x[i] : 0.0);
+      sum -= 4 * kCat256;
+    }
+    return sum;
+  });
+  n = count;
+  last = count ? cat_key(end_t, end_i) : 0;
+  return w;
+}
+
+// Writes a row's summary and draws its token.  listed < kept.n: the pieces' sums are in seg.
+template <typename T>
+__device__ __forceinline__ void cat_finish(CatShared& sh, const CatParams& p, int64_t r, const CatRow<T>& row, const u64* seg, float inv_t, const CatScale& sc, float m, const CatKept& kept) {
+  const int tid = threadIdx.x;
+  const double norm = static_cast<double>(m) + log(static_cast<double>(kept.w)) - 44.0 * 0.69314718055994530942;
+  const CatBound bound{cat_key_value(kept.last), static_cast<int>(static_cast<uint32_t>(kept.last))};
+  if (tid == 0 && p.dist) {
+    double* d = p.dist + r * kCatRow;
+    d[0] = norm; d[1] = bound.value; d[2] = bound.idx; d[3] = static_cast<double>(kept.n); d[4] = inv_t;
+  }
+  if (!p.u) return;
+  const u64 target = cat_target(p.u[r], kept.w);
+  int found = -1;
+  if (kept.listed == static_cast<int>(kept.n) && kept.listed <= kCatThreads) {   // all of them are listed: each adds up those of smaller index
+    const int n = kept.listed;
+    u64* w = reinterpret_cast<u64*>(sh.hist);
+    __syncthreads();
+    const u64 own = tid < n ? cat_weight(cat_key_value(sh.list[tid]), sc, sh.tab) : 0;
+    w[tid] = own;
+    __syncthreads();
+    if (tid < n) {
+      const uint32_t idx = static_cast<uint32_t>(sh.list[tid]);
+      u64 before = 0;
+      for (int j = 0; j < n; ++j) before += static_cast<uint32_t>(sh.list[j]) < idx ? w[j] : 0;
+      if (before < target && before + own >= target) found = static_cast<int>(idx);
+    }
+  } else {
+    found = cat_locate(sh, row, seg, target, kept.listed, [&](u64 key) { return cat_weight(cat_key_value(key), sc, sh.tab); }, [&](float l, int idx) -> u64 {
+      const float t = cat_scale(l, inv_t);
+      return bound.kept(t, idx) ? cat_weight(t, sc, sh.tab) : 0;
+    });
+  }
+  if (found >= 0) {
+    p.token[r] = found;
+    if (p.logp) p.logp[r] = static_cast<float>(static_cast<double>(cat_scale(cat_float(row.base[row.head + found]), inv_t)) - norm);
+  }
+}
+
+// A row by one block, whatever it holds.
+template <typename T>
+__device__ __noinline__ void cat_search(CatShared& sh, const CatParams& p, int64_t r, const CatRow<T>& row, u64* seg, const CatRequest& q, bool by_k, const CatScale& sc, float m) {
+  constexpr int kVec = CatRow<T>::kVec;
+  const int pieces = row.pieces();
+  u64 cut = ~0ull;
+  if (by_k) cut = cat_refine<false>(sh, row, q.inv_t, sc, cut, q.want, 0.0);
+  if (q.by_p) {
+    u64 w = 0, none = 0, none2 = 0;
+    cat_each(row, 0, pieces, [&](const float* l, int idx) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float t = cat_scale(l[i], q.inv_t);
+        if (cat_key(t, idx + i) <= cut) w += cat_weight(t, sc, sh.tab);
+      }
+    });
+    cat_reduce(sh, w, none, none2);
+    cut = cat_refine<true>(sh, row, q.inv_t, sc, cut, 0, cat_limit(q.top_p, w));
+  }
+  const float least = cat_least(p, r, m);
+  CatBound bound{-INFINITY, INT_MIN};          // (everything that is not masked)
+  if (cut != ~0ull) bound = CatBound{cat_key_value(cut), static_cast<int>(static_cast<uint32_t>(cut))};
+  if (bound.value < least) bound = CatBound{least, INT_MAX};
+  CatKept kept{};
+  u64 w = cat_keep(row, 0, pieces, seg, q.inv_t, sc, sh.tab, bound, kept.n, kept.last);
+  cat_reduce(sh, w, kept.n, kept.last);
+  kept.w = w;
+  __threadfence();
+  cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
+}
+
+// ------------------------------------------------------------------------------------------------------------- kernels
+// The largest logit of a part (scaling is monotonic: the largest scaled one is its scaled logit) and how many are not masked; for a
+// small top-k also a threshold above which that many tokens of the row lie for certain: this part's share of them, by its threads' own maxima.
+// Bound by reading the logits.
+template <typename T>
+__global__ void __launch_bounds__(kCatThreads) cat_top_kernel(const __grid_constant__ CatParams p) {
+  __shared__ uint2 part[kCatWarps];
+  const int tid = threadIdx.x, row_i = blockIdx.x / p.w.splits, split = blockIdx.x % p.w.splits;
+  const int64_t r = p.r0 + row_i;
+  constexpr int kVec = CatRow<T>::kVec, kU = 8;
+  griddep_enter();
+  const CatRequest q(p, r);
+  const CatRow<T> row(p.logits, r, p.V);
+  if (q.want || q.by_p) {   // the row's counts start at zero
+    uint4* h = reinterpret_cast<uint4*>(p.w.hist + static_cast<int64_t>(row_i) * 2 * kCatBins);
+    for (int i = split * kCatThreads + tid; i < 2 * kCatBins / 4; i += p.w.splits * kCatThreads) h[i] = make_uint4(0, 0, 0, 0);
+  }
+  if (split == 0 && tid == 0) {
+    CatState* st = p.w.state + row_i;
+    st->ticket[0] = st->ticket[1] = st->list_n = 0; st->mode = CAT_DONE;
+  }
+  float mine = -INFINITY;
+  uint32_t live = 0;
+  const int v1 = (split + 1) * p.w.share * (kCatPiece / kVec);
+  for (int v0 = split * p.w.share * (kCatPiece / kVec) + tid; v0 < v1; v0 += kU * kCatThreads) {
+    uint4 raw[kU];
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      const int v = v0 + j * kCatThreads;
+      raw[j] = row.none();
+      if (v < v1 && row.whole(v)) raw[j] = row.vec(v);
+    }
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      const int v = v0 + j * kCatThreads;
+      if (v < v1 && !row.whole(v) && row.some(v)) raw[j] = row.edge(v);
+      float l[kVec];
+      CatType<T>::unpack(raw[j], l);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) { mine = fmaxf(mine, l[i]); live += l[i] > -INFINITY; }
+    }
+  }
+  const uint32_t own = cat_ord(mine);
+  uint32_t tau = 0;
+  if (q.few) {
+    const int share = (q.want + p.w.splits - 1) / p.w.splits;
+    uint32_t lo = 0, hi = 0xff800000u;   // fewer than share at lo (none are that large), share at hi (if at all)
+    while (hi - lo > 1) {
+      const uint32_t at = lo + (hi - lo) / 2;
+      const int n = __syncthreads_count(own <= at);
+      if (n >= share) { hi = at; if (n <= share + share / 4 + 2) break; } else lo = at;
+    }
+    tau = hi;
+  }
+  const uint32_t top = __reduce_min_sync(0xffffffffu, own);
+  live = __reduce_add_sync(0xffffffffu, live);
+  if ((tid & 31) == 0) part[tid >> 5] = make_uint2(top, live);
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t a = 0xffffffffu, n = 0;
+    for (int i = 0; i < kCatWarps; ++i) { a = min(a, part[i].x); n += part[i].y; }
+    p.w.top[static_cast<int64_t>(row_i) * p.w.splits + split] = CatTop{a, tau, n, 0};
+  }
+}
+
+// From a row's counts: between which bins top-p ends, and in which top-k; what cat_range_kernel has to look at.
+__device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatState* st, const CatRequest& q, uint32_t live, float m, float least) {
+  const int tid = threadIdx.x;
+  constexpr int kEach = kCatBins / kCatThreads;
+  const bool by_k = q.want > 0 && static_cast<uint32_t>(q.want) < live;
+  const uint32_t k = q.want;
+  uint32_t n[kEach], own_n = 0;
+  float e[kEach], own_e = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kEach; j += 4) {
+    const uint4 h = __ldcg(reinterpret_cast<const uint4*>(hist) + (tid * kEach + j) / 4);
+    const uint4 f = __ldcg(reinterpret_cast<const uint4*>(hist + kCatBins) + (tid * kEach + j) / 4);
+    const uint32_t hn[4] = {h.x, h.y, h.z, h.w}, fn[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      n[j + i] = hn[i];
+      const float c = static_cast<float>(hn[i]);
+      const float place = tid * kEach + j + i + (hn[i] ? __fdividef(static_cast<float>(fn[i]), c * (1 << kCatFrac)) : 0.0f);
+      e[j + i] = q.by_p ? c * exp2f(-static_cast<float>(kLog2e) / kCatPerUnit * place) : 0.0f;
+      own_n += n[j + i]; own_e += e[j + i];
+    }
+  }
+  uint32_t cum0 = own_n;
+  float mass0 = own_e, all_mass;
+  if (tid == 0) { sh.found_a = sh.found_b = sh.found_k = kCatBins; sh.found_prev = -1; }
+  cat_block_scan2(cum0, mass0, sh.scan2, &all_mass);
+  cum0 -= own_n; mass0 -= own_e;
+  // the bin in which top-k ends, and bounds of the weight that top-p refers to
+  float lo = all_mass, hi = all_mass;
+  if (by_k) {
+    uint32_t cum = cum0;
+    float mass = mass0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (cum < k && cum + n[j] >= k) {
+        sh.found_k = tid * kEach + j;
+        const float w = e[j] / n[j] * (k - cum);   // a part of the bin: weights within exp(+-1/64)
+        sh.found_lo = mass + w * 0.984f; sh.found_hi = mass + w * 1.016f;
       }
       cum += n[j]; mass += e[j];
     }
     __syncthreads();
-    int bin_a = sh.found_a, bin_b = sh.found_b;
-    int upto = sh.found_n;
-    if (!k_counts && !p_all && live <= kCatList) { bin_b = 4096; upto = static_cast<int>(live); }   // all of them, sorted
-    const bool found = bin_b != kCatBins;
-    if (found && upto <= kCatList) {
-      listed = true;
-      cat_each(row, part, inv_t, 0, part.iters, [&](const float* t, int idx) {
+    lo = sh.found_lo; hi = sh.found_hi;
+  }
+  const int bin_k = sh.found_k;
+  int bin_a = bin_k, bin_b = bin_k;
+  if (q.by_p) {
+    // A bin's weight is its count times the weight at its tokens' mean place, to (1/64)^2 / 8 = 2^-15 (its tokens' weights are within
+    // exp(-1/64) of each other), 2^-12 / 64 and 2^-12 / 64 for the places' rounding, 2^-20 for the exponential's and the fp32 sums'.
+    constexpr float kLo = 1.0f - 4e-5f, kHi = 1.0f + 7e-5f;
+    constexpr float kNear = 1.0f + 1e-5f;   // (the sum up to a bin is not the same number at its end and at the next one's start)
+    const float lim_lo = q.top_p * lo * kLo, lim_hi = q.top_p * hi * kHi;
+    float mass = mass0;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
-          if (t[i] > -INFINITY && cat_bin(m, t[i]) <= bin_b) team.at(sh.list, 0)[atomicAdd(team.at(&sh.list_n, 0), 1u)] = cat_key(t[i], idx + i);
-      });
-      team.sync();
-      if (team.rank == 0) {
-        cat_sort(sh.list, upto);
-        constexpr int kEach = kCatList / kCatThreads;
-        u64 lw[kEach], s = 0;
+    for (int j = 0; j < kEach; ++j) {
+      const int b = tid * kEach + j;
+      const float end = j < kEach - 1 ? mass + e[j] : mass0 + own_e;
+      // top-p ends in the first bin at whose end its weight is reached: not before a, not behind b
+      if ((mass * kHi < lim_lo * kNear || b == 0) && end * kHi >= lim_lo) atomicMin(&sh.found_a, b);
+      if ((mass * kLo < lim_hi * kNear || b == 0) && end * kLo >= lim_hi) atomicMin(&sh.found_b, b);
+      mass = end;
+    }
+    __syncthreads();
+    bin_a = sh.found_a; bin_b = sh.found_b;
+    if (by_k && bin_b >= bin_k) { bin_b = bin_k; bin_a = min(bin_a, bin_k); }   // top-k's end lies among the bins of top-p's
+  }
+  bool ends = false;
+  if (least > -INFINITY) {
+    // min-p may end before: in the bin of its least logit, or in the last one before that holds any
+    const int bin_m = static_cast<int>(cat_place(m, least, 1.0f) >> kCatFrac);
+    if (bin_m <= bin_b && bin_m < kCatBins) {
+      ends = true;
+      bin_b = bin_m;
+      bin_a = min(bin_a, bin_m);
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int i = tid * kEach + j;
-          lw[j] = i < upto ? weight(cat_key_value(sh.list[i])) : 0;
-          s += lw[j];
-        }
-        u64 total;
-        const u64 start = cat_block_scan<u64>(s, sh.scan, &total) - s;
-        const int most = static_cast<int>(k_counts ? k : min(live, static_cast<u64>(upto)));
-        u64 before = start;
-        if (tid == 0) sh.found_sum = total;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) { before += lw[j]; if (k_counts && tid * kEach + j == most - 1) sh.found_sum = before; }
-        __syncthreads();
-        const double lim = by_p ? (p_all ? limit : cat_limit(tp, sh.found_sum)) : INFINITY;
-        before = start;
-        int mine = 0;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int i = tid * kEach + j;
-          mine += i < most && (i == 0 || (static_cast<double>(before) < lim && likely(cat_key_value(sh.list[i]))));
-          before += lw[j];
-        }
-        u64 all;
-        cat_block_scan<u64>(static_cast<u64>(mine), sh.scan, &all);
-        const int last = static_cast<int>(all) - 1;
-        before = start;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          before += lw[j];
-          if (tid * kEach + j == last) { sh.found_key = sh.list[last]; sh.found_count = all; sh.found_sum = before; }
-        }
-      }
-      team.sync();
-      cut = *team.at(&sh.found_key, 0);
-      kept_n = *team.at(&sh.found_count, 0);
-      kept_w = *team.at(&sh.found_sum, 0);
-      kept_last = cut;
-    } else {
-      // many candidates (wide top-k, flat distributions, many equals)
-      auto edge_a = [&](int b) { return b <= 0 ? 0ull : cat_key(nextafterf(nextafterf(m - (b - 0.02f) / kCatPerUnit, INFINITY), INFINITY), 0); };
-      auto edge_b = [&](int b) { return b >= kCatBins - 1 ? ~0ull : cat_key(nextafterf(nextafterf(m - (b + 1.02f) / kCatPerUnit, -INFINITY), -INFINITY), -1); };
-      if (k_counts) {
-        cut = cat_refine<false>(team, row, part, inv_t, m, c, edge_a(bin_a), edge_b(bin_b), ~0ull, k, 0.0);
-        bin_a = 0;
-      }
-      if (by_p) {
-        u64 w = sum;
-        if (k_counts || !with_sum) {
-          u64 x = 0, y = 0;
-          w = 0;
-          cat_each(row, part, inv_t, 0, part.iters, [&](const float* t, int idx) {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-              if (t[i] > -INFINITY && cat_key(t[i], idx + i) <= cut) w += weight(t[i]);
-          });
-          team.reduce(w, x, y);
-        }
-        const u64 a = p_all ? edge_a(bin_a) : 0;
-        u64 b = p_all ? edge_b(bin_b) : cut;
-        b = b < cut ? b : cut;
-        cut = cat_refine<true>(team, row, part, inv_t, m, c, a < b ? a : 0, b, cut, 0, cat_limit(tp, w));
-      }
+      for (int j = 0; j < kEach; ++j) if (n[j] && tid * kEach + j < bin_a) atomicMax(&sh.found_prev, tid * kEach + j);
+      __syncthreads();
+      if (sh.found_prev >= 0) bin_a = sh.found_prev;
     }
   }
-  auto kept_weight = [&](float t, int idx) -> u64 { return t > -INFINITY && cat_key(t, idx) <= cut && likely(t) ? weight(t) : 0; };
-  const bool pairs = listed && kept_n <= kCatPairs;
-  if (!listed || (p.u && !pairs)) {
-    u64 n = 0, last = 0;
-    u64 w = cat_sums(team, row, part, inv_t, [&](float t, int idx) -> u64 {
-      if (!(t > -INFINITY)) return 0;
-      const u64 key = cat_key(t, idx);
-      if (key > cut || !likely(t)) return 0;
-      ++n;
-      last = key > last ? key : last;
-      return weight(t);
+  const bool known = bin_b < kCatBins && bin_a <= bin_b && (!by_k || bin_k < kCatBins || (ends && !q.by_p));
+  uint32_t cum = cum0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int b = tid * kEach + j;
+    if (b == bin_a) sh.at_a = cum;
+    if (b == bin_k) sh.at_k = cum;
+    cum += n[j];
+    if (b == bin_b) sh.at_b = cum;
+    if (b == bin_k) sh.end_k = cum;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    const bool apart = by_k && q.by_p && bin_k > bin_b;   // top-k ends in a bin of its own, and top-p refers to what is before
+    st->mode = CAT_SEARCH;
+    if (known && sh.at_b - sh.at_a + (apart ? sh.end_k - sh.at_k : 0) <= kCatList) {
+      st->mode = CAT_RANGE;
+      st->ua = static_cast<uint32_t>(bin_a) << kCatFrac; st->ub = static_cast<uint32_t>(bin_b + 1) << kCatFrac;
+      st->uk = static_cast<uint32_t>(by_k ? bin_k : kCatBins) << kCatFrac; st->ue = st->uk + (apart ? 1u << kCatFrac : 0u);
+      st->at_a = sh.at_a; st->n1 = sh.at_b - sh.at_a; st->n_mid = apart ? sh.at_k - sh.at_b : 0;
+      st->apart = apart; st->upto = q.by_p && (apart || !by_k); st->ends = ends;
+    }
+  }
+}
+
+// Rows without top-k and top-p: everything that is left to do.  Rows with a small top-k: the tokens above the threshold, of which the
+// row's last block derives everything.  Other rows: counts by distance from the largest.
+template <typename T>
+__global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_constant__ CatParams p) {
+  __shared__ CatShared sh;
+  const int tid = threadIdx.x, row_i = blockIdx.x / p.w.splits, split = blockIdx.x % p.w.splits;
+  const int64_t r = p.r0 + row_i;
+  constexpr int kVec = CatRow<T>::kVec;
+  griddep_enter();
+  const CatRequest q(p, r);
+  const CatRow<T> row(p.logits, r, p.V);
+  if (tid == 0) sh.list_n = 0;
+  cat_table(sh.tab);
+  const CatTop top = cat_tops(sh, p.w, row_i);
+  if (top.live == 0) {   // nothing is left
+    if (split == 0 && tid == 0) {
+      if (p.dist) { double* d = p.dist + r * kCatRow; d[0] = -INFINITY; d[1] = INFINITY; d[2] = -1.0; d[3] = 0.0; d[4] = q.inv_t; }
+      if (p.u) { p.token[r] = -1; if (p.logp) p.logp[r] = -INFINITY; }
+    }
+    return;
+  }
+  const float m = cat_scale(cat_key_value(static_cast<u64>(top.top) << 32), q.inv_t);
+  const bool by_k = q.want > 0 && static_cast<uint32_t>(q.want) < top.live;
+  CatState* st = p.w.state + row_i;
+  u64* seg = p.w.seg + static_cast<int64_t>(row_i) * p.w.pieces;
+  const int p0 = split * p.w.share, p1 = min(p0 + p.w.share, row.pieces());
+  if (!by_k && !q.by_p) {
+    const CatScale sc(m, kCatFloor);
+    const float least = cat_least(p, r, m);
+    CatKept kept{};
+    u64 w = cat_keep(row, p0, p1, seg, q.inv_t, sc, sh.tab, least > -INFINITY ? CatBound{least, INT_MAX} : CatBound{-INFINITY, INT_MIN}, kept.n, kept.last);
+    cat_reduce(sh, w, kept.n, kept.last);
+    u64* tot = p.w.tot + static_cast<int64_t>(row_i) * p.w.splits * 3;
+    if (tid == 0) { __stcg(tot + split * 3, w); __stcg(tot + split * 3 + 1, kept.n); __stcg(tot + split * 3 + 2, kept.last); }
+    if (!cat_last(sh, &st->ticket[0], p.w.splits)) return;
+    w = 0; kept.n = 0; kept.last = 0;
+    for (int i = tid; i < p.w.splits; i += kCatThreads) {
+      w += __ldcg(tot + i * 3); kept.n += __ldcg(tot + i * 3 + 1);
+      const u64 k = __ldcg(tot + i * 3 + 2);
+      kept.last = k > kept.last ? k : kept.last;
+    }
+    cat_reduce(sh, w, kept.n, kept.last);
+    kept.w = w;
+    cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
+  } else if (by_k && q.few && top.tau < 0xff800000u) {
+    const float from = cat_key_value(static_cast<u64>(top.tau) << 32);
+    cat_each(row, p0, p1, [&](const float* l, int idx) {
+      float big = l[0];
+#pragma unroll
+      for (int i = 1; i < kVec; ++i) big = fmaxf(big, l[i]);
+      if (big >= from) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) if (l[i] >= from) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+      }
     });
-    team.reduce(w, n, last);
-    kept_n = n; kept_w = w; kept_last = last;
-  }
-  const double norm = md + log(static_cast<double>(kept_w)) - 44.0 * 0.69314718055994530942;
-  if (team.rank == 0 && tid == 0 && dist) {
-    dist[0] = norm; dist[1] = cat_key_value(kept_last); dist[2] = static_cast<double>(static_cast<uint32_t>(kept_last)); dist[3] = static_cast<double>(kept_n); dist[4] = inv_t;
-  }
-  if (p.u) {
-    const u64 target = cat_target(p.u[r], kept_w);
-    int found = -1;
-    if (pairs) {
-      if (team.rank == 0) {
-        const int n = static_cast<int>(kept_n);
-        __syncthreads();
-        u64* w = sh.list + kCatList - kCatPairs;   // (the list's own first kept_n entries stay)
-        if (tid < n) w[tid] = weight(cat_key_value(sh.list[tid]));
-        __syncthreads();
-        if (tid < n) {
-          const uint32_t idx = static_cast<uint32_t>(sh.list[tid]);
-          u64 before = 0;
-          for (int j = 0; j < n; ++j) before += static_cast<uint32_t>(sh.list[j]) < idx ? w[j] : 0;
-          if (before < target && before + w[tid] >= target) found = static_cast<int>(idx);
-        }
+    u64* list = p.w.list + static_cast<int64_t>(row_i) * kCatList;
+    cat_put_list(sh, st, list, p.w.splits);
+    if (!cat_last(sh, &st->ticket[0], p.w.splits)) return;
+    const CatScale sc(m, kCatFloor);
+    CatCut x{};
+    CatKept kept{};
+    x.n = x.n1 = cat_get_list(sh, st, list, p.w.splits);
+    x.by_k = true; x.by_p = q.by_p; x.k = q.want; x.top_p = q.top_p; x.least = cat_least(p, r, m);
+    if (x.n <= kCatList && cat_resolve(sh, x, sc, kept)) cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
+    else cat_search(sh, p, r, row, seg, q, by_k, sc, m);   // (many tokens above the threshold: rows in order, many equals)
+  } else {
+    for (int i = tid; i < 2 * kCatBins; i += kCatThreads) sh.hist[i] = 0;
+    __syncthreads();
+    cat_each(row, p0, p1, [&](const float* l, int) {
+      uint32_t at[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) at[i] = cat_place(m, l[i], q.inv_t);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) if (at[i] < (kCatBins << kCatFrac)) atomicAdd(&sh.hist[at[i] >> kCatFrac], 1u);
+      if (q.by_p) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) if (at[i] < (kCatBins << kCatFrac)) atomicAdd(&sh.hist[kCatBins + (at[i] >> kCatFrac)], at[i] & ((1u << kCatFrac) - 1));
       }
-    } else {
-      cat_locate(team, row, part, inv_t, target, kept_weight, &found);
-    }
-    if (found >= 0) {
-      p.token[r] = found;
-      if (p.logp) p.logp[r] = static_cast<float>(static_cast<double>(cat_scale(cat_float(row.base[row.head + found]), inv_t)) - norm);
-    }
+    });
+    __syncthreads();
+    uint32_t* hist = p.w.hist + static_cast<int64_t>(row_i) * 2 * kCatBins;
+    for (int i = tid; i < 2 * kCatBins; i += kCatThreads) if (sh.hist[i]) atomicAdd(hist + i, sh.hist[i]);
+    if (!cat_last(sh, &st->ticket[0], p.w.splits)) return;
+    cat_bins(sh, hist, st, q, top.live, m, cat_least(p, r, m));
   }
-  team.sync();   // no block leaves while another may still read its shared memory
+}
+
+// What cat_scan_kernel left: the weights above the bins in question (all weights where top-p refers to the whole row), piece by
+// piece, and the tokens of those bins, of which the row's last block derives the cut.  Bound by the exponentials: 4 cycles a warp of tokens in fp64.
+template <typename T>
+__global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_constant__ CatParams p) {
+  __shared__ CatShared sh;
+  const int tid = threadIdx.x, row_i = blockIdx.x / p.w.splits, split = blockIdx.x % p.w.splits;
+  const int64_t r = p.r0 + row_i;
+  constexpr int kVec = CatRow<T>::kVec;
+  griddep_enter();
+  CatState* st = p.w.state + row_i;
+  const int mode = st->mode;
+  if (mode == CAT_DONE || (mode == CAT_SEARCH && split > 0)) return;
+  const CatRequest q(p, r);
+  const CatRow<T> row(p.logits, r, p.V);
+  if (tid == 0) sh.list_n = 0;
+  cat_table(sh.tab);
+  const CatTop top = cat_tops(sh, p.w, row_i);
+  const float m = cat_scale(cat_key_value(static_cast<u64>(top.top) << 32), q.inv_t);
+  const bool by_k = q.want > 0 && static_cast<uint32_t>(q.want) < top.live;
+  u64* seg = p.w.seg + static_cast<int64_t>(row_i) * p.w.pieces;
+  const CatScale sc(m, kCatFloor);
+  if (mode == CAT_SEARCH) {
+    cat_search(sh, p, r, row, seg, q, by_k, sc, m);
+    return;
+  }
+  const uint32_t ua = st->ua, ub = st->ub, uk = st->uk, ue = st->ue;
+  const bool upto = st->upto != 0;
+  const uint32_t need = upto ? uk : ua;
+  const int p0 = split * p.w.share, p1 = min(p0 + p.w.share, row.pieces());
+  u64 w_upto = 0, none = 0;
+  u64 w_above = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+    u64 above = 0;
+    uint32_t at[kVec];
+    bool list = false;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      at[i] = cat_place(m, l[i], q.inv_t);
+      list = list || at[i] - ua < ub - ua || at[i] - uk < ue - uk;
+    }
+#pragma unroll
+    for (int h = 0; h < kVec; h += 4) {   // four exponentials side by side
+      if (!__any_sync(0xffffffffu, min(min(at[h], at[h + 1]), min(at[h + 2], at[h + 3])) < need)) continue;
+      double x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = sc.exp(__fmul_rn(l[h + i], q.inv_t), sh.tab);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) above += cat_bits(at[h + i] < ua ? x[i] : 0.0);
+      above -= 4 * kCat256;
+      if (upto) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w_upto += cat_bits(at[h + i] < uk ? x[i] : 0.0);
+        w_upto -= 4 * kCat256;
+      }
+    }
+    if (list) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        if (at[i] - ua < ub - ua || at[i] - uk < ue - uk) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+    }
+    return above;
+  });
+  cat_reduce(sh, w_above, w_upto, none);
+  u64* tot = p.w.tot + static_cast<int64_t>(row_i) * p.w.splits * 3;
+  if (tid == 0) { __stcg(tot + split * 3, w_above); __stcg(tot + split * 3 + 1, w_upto); }
+  u64* list = p.w.list + static_cast<int64_t>(row_i) * kCatList;
+  cat_put_list(sh, st, list, p.w.splits);
+  if (!cat_last(sh, &st->ticket[1], p.w.splits)) return;
+  w_above = 0; w_upto = 0;
+  for (int i = tid; i < p.w.splits; i += kCatThreads) { w_above += __ldcg(tot + i * 3); w_upto += __ldcg(tot + i * 3 + 1); }
+  cat_reduce(sh, w_above, w_upto, none);
+  CatCut x{};
+  CatKept kept{};
+  x.n = cat_get_list(sh, st, list, p.w.splits);
+  x.n1 = static_cast<int>(st->n1); x.n_above = st->at_a; x.n_mid = st->n_mid; x.w_above = w_above; x.w_upto = w_upto;
+  x.by_k = by_k; x.by_p = q.by_p; x.apart = st->apart != 0; x.ends = st->ends != 0; x.k = q.want; x.top_p = q.top_p; x.least = cat_least(p, r, m);
+  if (x.n <= kCatList && cat_resolve(sh, x, sc, kept)) cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
+  else cat_search(sh, p, r, row, seg, q, by_k, sc, m);
 }
 
 // ------------------------------------------------------------------------------------------------------- verification
@@ -744,72 +1186,146 @@ __global__ void __launch_bounds__(128) cat_verify_kernel(const CatVerifyParams p
 
 // --------------------------------------------------------------------------------------------------------- resampling
 struct CatResampleParams {
-  int B, gamma, rows, V;
+  int gamma, rows, V, splits, share, pieces;
+  int b0;                                   // first sequence of this launch
   CatView q, p;
   const double *dist_q, *dist_p;
   const int32_t* n_accept;
   const float* w;
   int32_t* x_new;
+  CatState* state;                          // [sequences]: tickets, zero between calls
+  u64 *seg, *tot;                           // [sequences, pieces], [sequences, splits]
 };
 
-// A cluster per sequence: the token of max(0, p - q) at the first rejected position (of p where that is nothing, and at the bonus
-// position).  Probabilities to 2^-52, integer sums as above.
+// The token of max(0, p - q) at the first rejected position (of p where that is nothing, and at the bonus position): probabilities to 2^-52,
+// integer sums by piece over (sequence, part of the row); the last block of a sequence finds the token.
 template <typename TQ, typename TP>
-__global__ void __launch_bounds__(kCatThreads, 2) cat_resample_kernel(const CatResampleParams p) {
+__global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __grid_constant__ CatResampleParams p) {
   __shared__ CatShared sh;
-  CatTeam team(sh);
-  const int b = blockIdx.x / team.cs;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i_b = blockIdx.x / p.splits, split = blockIdx.x % p.splits, b = p.b0 + i_b;
   griddep_enter();
   cat_table(sh.tab);
   __syncthreads();
   const int n = p.n_accept[b];
   const bool residual = n < p.gamma;
   const int64_t rp = static_cast<int64_t>(b) * p.rows + n, rq = static_cast<int64_t>(b) * p.gamma + n;
-  if (n < 0 || n >= p.rows || !(p.dist_p[rp * kCatRow + 3] > 0.0)) {   // (the whole cluster)
-    if (team.rank == 0 && threadIdx.x == 0) p.x_new[b] = -1;
-    team.sync();
+  if (n < 0 || n >= p.rows || !(p.dist_p[rp * kCatRow + 3] > 0.0)) {
+    if (split == 0 && tid == 0) p.x_new[b] = -1;
     return;
   }
   const double* dp = p.dist_p + rp * kCatRow;
-  const double cp = -dp[0] * kLog2e;
-  const float cut_p = static_cast<float>(dp[1]), inv_p = static_cast<float>(dp[4]);
-  const int last_p = static_cast<int>(dp[2]);
-  double cq = 0.0;
-  float cut_q = INFINITY, inv_q = 1.0f;
-  int last_q = -1;
+  const CatScale sp(dp[0], 42.0f);             // probabilities below 2^-60 count as that: 0 once rounded
+  const float inv_p = static_cast<float>(dp[4]);
+  const CatBound kept_p{static_cast<float>(dp[1]), static_cast<int>(dp[2])};
+  double norm_q = 0.0;
+  CatBound kept_q{INFINITY, INT_MIN};
+  float inv_q = 1.0f;
   if (residual) {
     const double* dq = p.dist_q + rq * kCatRow;
-    if (dq[3] > 0.0) { cq = -dq[0] * kLog2e; cut_q = static_cast<float>(dq[1]); last_q = static_cast<int>(dq[2]); }
+    if (dq[3] > 0.0) { norm_q = dq[0]; kept_q = CatBound{static_cast<float>(dq[1]), static_cast<int>(dq[2])}; }
     inv_q = static_cast<float>(dq[4]);
   }
+  const CatScale sq(norm_q, 42.0f);
   const CatRow<TP> row(p.p, rp, p.V);
-  const TQ* qrow = static_cast<const TQ*>(p.q.data) + (residual ? rq * p.q.ld : 0);
-  const CatPart part(row, team.cs, team.rank);
-  bool minus = residual;
-  auto kept = [](float t, int i, float cut, int last) { return t > cut || (t == cut && i <= last); };
-  auto weight = [&](float t, int idx) -> u64 {
-    if (!(t > -INFINITY) || !kept(t, idx, cut_p, last_p)) return 0;
-    double x = cat_exp(fmaxf(t, -FLT_MAX), cp, sh.tab);
-    if (static_cast<double>(t) * kLog2e + cp < -60.0) x = 0.0;
-    if (minus) {
-      const float tq = cat_scale(cat_float(qrow[idx]), inv_q);
-      if (kept(tq, idx, cut_q, last_q) && static_cast<double>(tq) * kLog2e + cq > -60.0) x -= cat_exp(tq, cq, sh.tab);
+  const CatRow<TQ> qrow(p.q, residual ? rq : 0, p.V);
+  constexpr int kVec = CatRow<TP>::kVec;
+  // a vector's weight; y: the draft's logits of the same tokens
+  auto weights = [&](const float* x, const float* y, int idx, bool minus) -> u64 {
+    u64 sum = 0;
+#pragma unroll
+    for (int h = 0; h < kVec; h += 4) {     // four exponentials side by side
+      double a[4];
+      bool in[4], any = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { in[i] = kept_p.kept(cat_scale(x[h + i], inv_p), idx + h + i); any = any || in[i]; }
+      if (!__any_sync(0xffffffffu, any)) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = sp.exp(__fmul_rn(x[h + i], inv_p), sh.tab);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = in[i] ? a[i] : 0.0;
+      if (minus) {
+        double d[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = sq.exp(__fmul_rn(y[h + i], inv_q), sh.tab);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] -= kept_q.kept(cat_scale(y[h + i], inv_q), idx + h + i) ? d[i] : 0.0;
+      }
+      // 1 added: the bits behind 1's are the value in units of 2^-52
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += static_cast<u64>(__double_as_longlong(fmax(a[i], 0.0) + 1.0));
+      sum -= 4 * 0x3ff0000000000000ull;
     }
-    return x > 0.0 ? static_cast<u64>(__double_as_longlong(x + 1.0) - __double_as_longlong(1.0)) : 0;
+    return sum;
   };
-  u64 total;
-  for (;;) {
-    u64 none = 0, more = 0;
-    total = cat_sums(team, row, part, inv_p, weight);
-    team.reduce(total, none, more);
-    if (total > 0 || !minus) break;
+  // sums of pieces [p0, p1); this thread's own
+  u64* seg = p.seg + static_cast<int64_t>(i_b) * p.pieces;
+  auto pass = [&](int p0, int p1, bool minus) -> u64 {
+    if (minus && sizeof(TQ) == sizeof(TP) && qrow.head == row.head) {   // rows that lie alike: both as vectors
+      constexpr int kIts = kCatPiece / (32 * kVec);
+      u64 all = 0;
+      for (int g = p0 + warp; g < p1; g += kCatWarps) {
+        u64 sum = 0;
+#pragma unroll
+        for (int h = 0; h < kIts; h += 2) {
+          uint4 a[2], d[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int v = (g * kIts + h + j) * 32 + lane;
+            if (row.whole(v)) { a[j] = row.vec(v); d[j] = qrow.vec(v); }
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int v = (g * kIts + h + j) * 32 + lane;
+            if (!row.whole(v)) { a[j] = row.some(v) ? row.edge(v) : row.none(); d[j] = row.some(v) ? qrow.edge(v) : qrow.none(); }
+            float x[kVec], y[CatRow<TQ>::kVec > kVec ? CatRow<TQ>::kVec : kVec];
+            CatType<TP>::unpack(a[j], x);
+            CatType<TQ>::unpack(d[j], y);
+            sum += weights(x, y, v * kVec - row.head, true);
+          }
+        }
+        all += sum;
+        sum = cat_warp_sum(sum);
+        if (lane == 0) seg[g] = sum;
+      }
+      return all;
+    }
+    return cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+      float y[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) y[i] = minus && idx + i >= 0 && idx + i < p.V ? cat_float(qrow.base[qrow.head + idx + i]) : -INFINITY;
+      return weights(l, y, idx, minus);
+    });
+  };
+  const int p0 = split * p.share, p1 = min(p0 + p.share, row.pieces());
+  u64 total = pass(p0, p1, residual), none = 0, none2 = 0;
+  cat_reduce(sh, total, none, none2);
+  u64* tot = p.tot + static_cast<int64_t>(i_b) * p.splits;
+  if (tid == 0) __stcg(tot + split, total);
+  uint32_t* ticket = &p.state[i_b].ticket[0];
+  if (!cat_last(sh, ticket, p.splits)) return;
+  if (tid == 0) *ticket = 0;                // for the next call
+  total = 0;
+  for (int i = tid; i < p.splits; i += kCatThreads) total += __ldcg(tot + i);
+  cat_reduce(sh, total, none, none2);
+  bool minus = residual;
+  if (total == 0 && minus) {                // p = q as far as 2^-52 goes: of p, by this block alone
     minus = false;
-    team.sync();
+    total = pass(0, row.pieces(), false);
+    cat_reduce(sh, total, none, none2);
+    __threadfence();
   }
-  int found = -1;
-  if (total > 0) cat_locate(team, row, part, inv_p, cat_target(p.w[b], total), weight, &found);
+  if (total == 0) return;
+  const int found = cat_locate(sh, row, seg, cat_target(p.w[b], total), 0, [](u64) -> u64 { return 0; }, [&](float l, int idx) -> u64 {
+    const float t = cat_scale(l, inv_p);
+    if (!kept_p.kept(t, idx)) return 0;
+    double a = sp.exp(t, sh.tab);
+    if (minus) {
+      const float tq = cat_scale(cat_float(qrow.base[qrow.head + idx]), inv_q);
+      if (kept_q.kept(tq, idx)) a -= sq.exp(tq, sh.tab);
+    }
+    return static_cast<u64>(__double_as_longlong(fmax(a, 0.0) + 1.0) - 0x3ff0000000000000ll);
+  });
   if (found >= 0) p.x_new[b] = found;
-  team.sync();
 }
 
 }  // namespace csd

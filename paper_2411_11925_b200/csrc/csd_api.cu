@@ -80,6 +80,7 @@ struct csd_ctx {
   HostIo gc[2];    // group chain kernel (per chain slot): s of all steps
   HostIo gm[2];    // group and wide chain kernels: condition products of two chunks of steps (wide: s of a chunk before them)
   HostIo wx[2];    // wide chain kernel: what its column tiles exchange
+  HostIo ct, cr;   // categorical heads: rows' states, counts, candidates and sums; tickets and sums of resampling
   size_t gc_refused[2] = {SIZE_MAX, SIZE_MAX}, gm_refused[2] = {SIZE_MAX, SIZE_MAX}, wc_refused[2] = {SIZE_MAX, SIZE_MAX};   // sizes that could not be had (wc: gm and wx of a wide chain): asked for again where the device has as much free
   cudaStream_t aux[2] = {nullptr, nullptr};        // (per chain slot) where they are formed
   cudaEvent_t ev_prep[2] = {}, ev_mods[2][2] = {}, ev_read[2][2] = {};   // preparation done; a chunk is written / has been read
@@ -1450,7 +1451,6 @@ template <typename TQ> auto cat_resample_pick_p(int dp) {
 auto cat_resample_pick(int dq, int dp) {
   return dq == CSD_F32 ? cat_resample_pick_p<float>(dp) : dq == CSD_BF16 ? cat_resample_pick_p<__nv_bfloat16>(dp) : cat_resample_pick_p<__half>(dp);
 }
-constexpr int kCatMaxV = 1 << 19;        // sums of 2^19 weights of 2^44 stay far below 2^64
 constexpr int kQuantMaxK = 1 << 20;
 
 int check_cat(csd_ctx* ctx, const csd_logits* l, const char* what) {
@@ -1477,35 +1477,76 @@ int check_cat_round(csd_ctx* ctx, int B, int gamma, int rows_p, int V) {
 
 CatView cat_view(const csd_logits* l) { return CatView{l->data, l->ld}; }
 
-// Blocks a row: as many as keep the device's SMs busy with two blocks each, none with less than 4096 tokens of its own.
-int cat_cluster(const csd_ctx* ctx, int64_t rows, int V) {
-  int cs = 1;
-  while (cs < kCatMaxCluster && rows * cs * 2 <= 2 * ctx->num_sms && V > 4096 * cs) cs *= 2;
-  return cs;
-}
-
-template <typename P>
-int launch_cat(csd_ctx* ctx, void (*kern)(P), int64_t rows, int cs, const P& p) {
-  cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3(static_cast<unsigned>(rows * cs)); lc.blockDim = dim3(kCatThreads); lc.stream = ctx->stream;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = static_cast<unsigned>(cs); at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-  lc.attrs = at; lc.numAttrs = 2;
-  CSD_CUDA(ctx, cudaLaunchKernelEx(&lc, kern, p));
-  ctx->launches++;
-  return CSD_OK;
+// Parts of the rows: so many that `rows` of them give every SM eight blocks, of 4096 to 32768 tokens each.
+void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int* splits, int* share, int* pieces) {
+  const int size = l->dtype == CSD_F32 ? 4 : 2, vec = 16 / size;
+  const bool aligned = reinterpret_cast<uintptr_t>(l->data) % 16 == 0 && (l->ld * size % 16 == 0 || rows == 1);
+  *pieces = (V + (aligned ? 0 : vec - 1) + kCatPiece - 1) / kCatPiece;
+  const int64_t want = (*pieces * rows + 8 * ctx->num_sms - 1) / (8 * ctx->num_sms);
+  *share = static_cast<int>(want < 8 ? 8 : want > 64 ? 64 : (want + 7) / 8 * 8);
+  *splits = (*pieces + *share - 1) / *share;
 }
 
 int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_cat_params* f, const float* u, int32_t* token, float* logp, double* dist) {
   CatParams p{};
-  p.R = static_cast<int>(R); p.V = V; p.logits = cat_view(l);
+  p.V = V; p.logits = CatView{l->data, l->ld};
   if (f) { p.temperature = f->temperature; p.top_k = f->top_k; p.top_p = f->top_p; p.min_p = f->min_p; }
   p.u = u; p.token = token; p.logp = logp; p.dist = dist;
-  auto kern = l->dtype == CSD_F32 ? cat_filter_kernel<float> : l->dtype == CSD_BF16 ? cat_filter_kernel<__nv_bfloat16> : cat_filter_kernel<__half>;
-  return launch_cat(ctx, kern, R, cat_cluster(ctx, R, V), p);
+  // Rows go in groups whose logits stay in L2 from one kernel to the next (64 MB of 126), and whose workspace is bounded.
+  const int64_t row_bytes = static_cast<int64_t>(V) * (l->dtype == CSD_F32 ? 4 : 2);
+  int64_t group = (int64_t(64) << 20) / row_bytes;
+  group = group < 1 ? 1 : group > 1024 ? 1024 : group;
+  const int64_t groups = (R + group - 1) / group;
+  group = (R + groups - 1) / groups;
+  CatWork& w = p.w;
+  cat_parts(ctx, group, l, V, &w.splits, &w.share, &w.pieces);
+  const bool cuts = f && (f->top_k || f->top_p || f->temperature);   // (zero temperature keeps one token)
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+  const size_t g = static_cast<size_t>(group);
+  const size_t o_state = take(g * sizeof(CatState)), o_top = take(g * w.splits * sizeof(CatTop)), o_seg = take(g * w.pieces * 8), o_tot = take(g * w.splits * 24);
+  const size_t o_hist = take(cuts ? g * 2 * kCatBins * 4 : 0), o_list = take(cuts ? g * kCatList * 8 : 0);
+  if (int rc = ensure_buffer(ctx, ctx->ct, off, "the rows of a categorical head")) return rc;
+  char* b = static_cast<char*>(ctx->ct.base);
+  w.state = reinterpret_cast<CatState*>(b + o_state); w.top = reinterpret_cast<CatTop*>(b + o_top);
+  w.seg = reinterpret_cast<u64*>(b + o_seg); w.tot = reinterpret_cast<u64*>(b + o_tot);
+  w.hist = reinterpret_cast<uint32_t*>(b + o_hist); w.list = reinterpret_cast<u64*>(b + o_list);
+  auto pick = [&](auto a, auto c, auto d) { return l->dtype == CSD_F32 ? a : l->dtype == CSD_BF16 ? c : d; };
+  for (int64_t r = 0; r < R; r += group) {
+    p.r0 = r;
+    w.rows = static_cast<int>(R - r < group ? R - r : group);
+    const unsigned grid = static_cast<unsigned>(w.rows * w.splits);
+    int rc = launch_short(ctx, ctx->stream, pick(cat_top_kernel<float>, cat_top_kernel<__nv_bfloat16>, cat_top_kernel<__half>), grid, kCatThreads, 0, p);
+    if (rc || (rc = launch_short(ctx, ctx->stream, pick(cat_scan_kernel<float>, cat_scan_kernel<__nv_bfloat16>, cat_scan_kernel<__half>), grid, kCatThreads, 0, p))) return rc;
+    if (cuts && (rc = launch_short(ctx, ctx->stream, pick(cat_range_kernel<float>, cat_range_kernel<__nv_bfloat16>, cat_range_kernel<__half>), grid, kCatThreads, 0, p))) return rc;
+  }
+  return CSD_OK;
+}
+
+int cat_resample(csd_ctx* ctx, int B, int gamma, int rows_p, int V, const csd_logits* q, const double* dist_q, const csd_logits* l, const double* dist_p,
+                 const int32_t* n_accept, const float* w, int32_t* x_new) {
+  CatResampleParams p{};
+  p.gamma = gamma; p.rows = rows_p; p.V = V; p.q = CatView{q->data, q->ld}; p.p = CatView{l->data, l->ld};
+  p.dist_q = dist_q; p.dist_p = dist_p; p.n_accept = n_accept; p.w = w; p.x_new = x_new;
+  const int group = B < 4096 ? B : 4096;
+  cat_parts(ctx, group, l, V, &p.splits, &p.share, &p.pieces);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+  const size_t g = static_cast<size_t>(group), o_seg = take(g * p.pieces * 8), o_tot = take(g * p.splits * 8);
+  // the tickets lie at the buffer's start at their most, so that no call's sums ever take their place: they are zero between calls
+  const size_t tickets = align_up(4096 * sizeof(CatState), 256);
+  const size_t had = ctx->cr.cap;
+  if (int rc = ensure_buffer(ctx, ctx->cr, tickets + off, "the sums of resampling")) return rc;
+  if (ctx->cr.cap != had) CSD_CUDA(ctx, cudaMemsetAsync(ctx->cr.base, 0, tickets, ctx->stream));
+  char* b = static_cast<char*>(ctx->cr.base);
+  p.state = reinterpret_cast<CatState*>(b);
+  p.seg = reinterpret_cast<u64*>(b + tickets + o_seg); p.tot = reinterpret_cast<u64*>(b + tickets + o_tot);
+  for (int s = 0; s < B; s += group) {
+    p.b0 = s;
+    const int n = B - s < group ? B - s : group;
+    if (int rc = launch_short(ctx, ctx->stream, cat_resample_pick(q->dtype, l->dtype), static_cast<unsigned>(n) * p.splits, kCatThreads, 0, p)) return rc;
+  }
+  return CSD_OK;
 }
 
 int check_quant(csd_ctx* ctx, const uint8_t* data, const uint8_t* scale, const char* what) {
@@ -1646,6 +1687,8 @@ int csd_destroy(csd_ctx* c) {
   for (HostIo& b : c->gc) if (b.base) cudaFree(b.base);
   for (HostIo& b : c->gm) if (b.base) cudaFree(b.base);
   for (HostIo& b : c->wx) if (b.base) cudaFree(b.base);
+  if (c->ct.base) cudaFree(c->ct.base);
+  if (c->cr.base) cudaFree(c->cr.base);
   if (c->d_err) cudaFree(c->d_err);
   cudaGetLastError();
   delete c;
@@ -2604,8 +2647,7 @@ int csd_cat_resample(csd_ctx* ctx, int B, int gamma, int rows_p, int V, const cs
   if (rc || (rc = check_cat(ctx, p, "target")) || (rc = check_cat_round(ctx, B, gamma, rows_p, V))) return rc;
   if (!dist_q || !dist_p || !n_accept || !w || !x_new) return fail(ctx, CSD_ERR_INVALID_ARG, "null array argument");
   CSD_DEVICE(ctx);
-  CatResampleParams r{B, gamma, rows_p, V, cat_view(q), cat_view(p), dist_q, dist_p, n_accept, w, x_new};
-  return launch_cat(ctx, cat_resample_pick(q->dtype, p->dtype), B, cat_cluster(ctx, B, V), r);
+  return cat_resample(ctx, B, gamma, rows_p, V, q, dist_q, p, dist_p, n_accept, w, x_new);
 }
 
 // ------------------------------------------------------------------ 8-bit matrices
