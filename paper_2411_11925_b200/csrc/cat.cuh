@@ -34,7 +34,6 @@ constexpr int kCatBins = 2048;        // bins of the histogram: 1/64 of scaled l
 constexpr float kCatPerUnit = 64.0f;
 constexpr int kCatFrac = 12;          // bits of a token's place within its bin: the places of 2^19 tokens add up to less than 2^32
 constexpr int kCatList = 2048;        // candidates that are sorted
-constexpr int kCatRank = 512;         // candidates up to which they are sorted by counting
 constexpr int kCatSub = 1024;         // bins of a refinement
 constexpr int kCatPiece = 512;        // tokens whose weights are summed together, to find a token by its cumulative weight
 constexpr int kCatRow = 5;            // doubles of a row's summary
@@ -288,7 +287,7 @@ struct CatShared {
   uint2 scan2[kCatWarps];
   u64 red[kCatWarps][3];
   double tab[16];
-  uint32_t rank[kCatRank];
+  uint32_t rank[2 * kCatThreads];             // of the sort
   CatTop top;
   // found by one thread, read by all
   u64 found_key, found_sum, found_upto, found_before[2];
@@ -339,35 +338,83 @@ __device__ __forceinline__ void cat_block_scan2(uint32_t& n, float& w, uint2* pa
   *total = all;
 }
 
-// Sorts list[0, n) ascending.  Up to kCatRank entries: each counts those before it, the block's threads sharing an entry's
-// count (a bitonic network is a round through shared memory a step: 10 k cycles for 256 entries, where this takes 1.5 k).  More: bitonic,
-// padded to a power of two; steps within 64 neighbours stay in one warp.
-__device__ __forceinline__ void cat_sort(CatShared& sh, int n) {
-  u64* list = sh.list;
-  const int tid = threadIdx.x;
-  if (n <= kCatRank) {
-    int P = 32;
-    while (P < n && P < kCatThreads) P <<= 1;
-    const int groups = kCatThreads / P, share = (n + groups - 1) / groups, from = tid / P * share, to = min(from + share, n);
-    const int o0 = tid & (P - 1), o1 = o0 + kCatThreads;
-    for (int i = tid; i < n; i += kCatThreads) sh.rank[i] = 0;
-    const u64 k0 = o0 < n ? list[o0] : ~0ull, k1 = o1 < n ? list[o1] : ~0ull;
-    uint32_t b0 = 0, b1 = 0;
-    if (n <= kCatThreads) {
-      for (int j = from; j < to; ++j) b0 += list[j] < k0;
-    } else {
-      for (int j = from; j < to; ++j) { const u64 x = list[j]; b0 += x < k0; b1 += x < k1; }
+// Sorts list[0, n) ascending: by value into 256 buckets of equal width, then by counting within each (1.2 k cycles at 400 entries; each counting
+// all before it took 11 k, a bitonic network, whose every step is a round through shared memory, 20 k).  Where a bucket
+// holds too many (equals) the network does it, padded to a power of two; steps within 64 neighbours stay in one warp.
+__device__ __noinline__ void cat_sort(CatShared& sh, int n) {
+  u64* const list = sh.list;
+  u64* const other = reinterpret_cast<u64*>(sh.hist);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int kEach = kCatList / kCatThreads, kMost = 64;
+  static_assert(kCatThreads == 256, "a thread a bucket");
+  const int each = (n + kCatThreads - 1) / kCatThreads;
+  sh.rank[tid] = 0;
+  uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if (j >= each) break;
+    const int i = tid + j * kCatThreads;
+    if (i < n) { const uint32_t o = static_cast<uint32_t>(list[i] >> 32); lo = min(lo, o); hi = max(hi, o); }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi);
+  if (lane == 0) sh.scan2[warp] = make_uint2(lo, hi);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kCatWarps; ++i) { const uint2 x = sh.scan2[i]; lo = min(lo, x.x); hi = max(hi, x.y); }
+  const float first = cat_key_value(static_cast<u64>(lo) << 32), last = cat_key_value(static_cast<u64>(hi) << 32);
+  const float width = fmaxf(first - last, FLT_MIN), scale = fminf(__fdividef(255.0f, width), FLT_MAX);
+  uint32_t at[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if (j >= each) break;
+    const int i = tid + j * kCatThreads;
+    if (i < n) {
+      const uint32_t b = min(__float2uint_rd(fminf((first - cat_key_value(list[i])) * scale, 255.0f)), 255u);
+      at[j] = b << 16 | atomicAdd(&sh.rank[b], 1u);
+    }
+  }
+  __syncthreads();
+  const uint32_t own = sh.rank[tid];
+  if (!__syncthreads_or(own > kMost)) {
+    uint32_t end = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const uint32_t x = __shfl_up_sync(0xffffffffu, end, o); if (lane >= o) end += x; }
+    if (lane == 31) sh.scan2[warp].x = end;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kCatWarps; ++i) if (i < warp) end += sh.scan2[i].x;
+    sh.rank[kCatThreads + tid] = end;                // where a bucket ends
+    __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if (j >= each) break;
+      const int i = tid + j * kCatThreads;
+      if (i < n) { const uint32_t b = at[j] >> 16; other[sh.rank[kCatThreads + b] - sh.rank[b] + (at[j] & 0xffffu)] = list[i]; }
     }
     __syncthreads();
-    if (o0 < n && b0) atomicAdd(&sh.rank[o0], b0);
-    if (o1 < n && b1) atomicAdd(&sh.rank[o1], b1);
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if (j >= each) break;
+      const int i = tid + j * kCatThreads;
+      if (i < n) {
+        const u64 key = list[i];
+        const uint32_t b = at[j] >> 16, to = sh.rank[kCatThreads + b], from = to - sh.rank[b];
+        uint32_t before = from;
+        for (uint32_t k = from; k < to; ++k) before += other[k] < key;
+        at[j] = before;
+      }
+    }
     __syncthreads();
-    if (tid < P && o0 < n) list[sh.rank[o0]] = k0;
-    if (o1 < n) list[sh.rank[o1]] = k1;
+    u64 key[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) { if (j >= each) break; const int i = tid + j * kCatThreads; if (i < n) key[j] = list[i]; }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) { if (j >= each) break; const int i = tid + j * kCatThreads; if (i < n) list[at[j]] = key[j]; }
     __syncthreads();
     return;
   }
-  int P = 1024;
+  int P = 128;
   while (P < n) P <<= 1;
   for (int i = n + tid; i < P; i += kCatThreads) list[i] = ~0ull;
   __syncthreads();
@@ -424,52 +471,70 @@ __device__ __forceinline__ u64 cat_target(float u, u64 total) {
 }
 
 // The token at which the cumulative weight reaches target, by one block: seg has the sums of all pieces, without the weights of
-// the first `extra` entries of the list; the piece that holds the token is gone through again.  weight(l, idx): of a logit, as in
-// the pass that formed the sums, listed tokens included.  One lane gets the token.
+// the first `extra` entries of the list (listed(key)); the piece that holds the token is gone through again, a warp a vector.
+// weights(l, idx, w): of a vector's logits, as in the pass that formed the sums, listed tokens included.  One thread gets the token, the others -1.
 template <typename T, typename W, typename L>
-__device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, const u64* seg, u64 target, int extra, L listed, W weight) {
-  constexpr int kVec = CatRow<T>::kVec, kEach = (kCatMaxPieces + kCatThreads - 1) / kCatThreads;
-  const int tid = threadIdx.x, lane = tid & 31, pieces = row.pieces(), each = (pieces + kCatThreads - 1) / kCatThreads;
-  u64* all = reinterpret_cast<u64*>(sh.hist);
-  __syncthreads();
-  for (int i = tid; i < pieces; i += kCatThreads) all[i] = __ldcg(seg + i);
+__device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, const u64* seg, u64 target, int extra, L listed, W weights) {
+  constexpr int kVec = CatRow<T>::kVec, kIts = kCatPiece / (32 * kVec), kEach = (kCatMaxPieces + kCatThreads - 1) / kCatThreads;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pieces = row.pieces(), each = (pieces + kCatThreads - 1) / kCatThreads;
+  // listed weights are added up in two words of 22 and 23 bits (a piece has 2^9 tokens)
+  uint32_t *lo = sh.hist, *hi = sh.hist + kCatMaxPieces;
   __syncthreads();
   if (extra > 0) {
+    for (int i = tid; i < pieces; i += kCatThreads) { lo[i] = 0; hi[i] = 0; }
+    __syncthreads();
     for (int i = tid; i < extra; i += kCatThreads) {
-      const u64 key = sh.list[i];
-      atomicAdd(&all[(static_cast<int>(static_cast<uint32_t>(key)) + row.head) / kCatPiece], listed(key));
+      const u64 key = sh.list[i], w = listed(key);
+      const int q = (static_cast<int>(static_cast<uint32_t>(key)) + row.head) / kCatPiece;
+      atomicAdd(&lo[q], static_cast<uint32_t>(w) & 0x3fffffu);
+      atomicAdd(&hi[q], static_cast<uint32_t>(w >> 22));
     }
     __syncthreads();
   }
-  u64 s = 0, total;
+  u64 x[kEach], s = 0, total;
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) if (j < each && tid * each + j < pieces) s += all[tid * each + j];
+  for (int j = 0; j < kEach; ++j) {
+    const int i = tid * each + j;
+    x[j] = 0;
+    if (j < each && i < pieces) {
+      x[j] = __ldcg(seg + i);
+      if (extra > 0) x[j] += lo[i] + (static_cast<u64>(hi[i]) << 22);
+    }
+    s += x[j];
+  }
   u64 before = cat_block_scan<u64>(s, sh.scan, &total) - s;
-  for (int j = 0; j < each; ++j) {
-    if (tid * each + j >= pieces) break;
-    const u64 x = all[tid * each + j];
-    if (before < target && before + x >= target) { sh.found_piece = tid * each + j; sh.found_sum = before; }
-    before += x;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if (before < target && before + x[j] >= target) { sh.found_piece = tid * each + j; sh.found_sum = before; }
+    before += x[j];
+  }
+  __syncthreads();
+  const int piece = sh.found_piece;
+  u64 w[kVec], incl = 0;
+  int idx = 0;
+  if (warp < kIts) {
+    const int v = (piece * kIts + warp) * 32 + lane;
+    uint4 raw = row.whole(v) ? row.vec(v) : row.some(v) ? row.edge(v) : row.none();
+    float l[kVec];
+    CatType<T>::unpack(raw, l);
+    idx = v * kVec - row.head;
+    weights(l, idx, w);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) incl += w[i];
+    s = incl;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const u64 y = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += y; }
+    if (lane == 31) sh.scan[warp] = incl;
   }
   __syncthreads();
   int token = -1;
-  if (tid < 32) {   // (the piece's first and only warp)
-    const int piece = sh.found_piece;
-    before = sh.found_sum;
-    cat_each(row, piece, piece + 1, [&](const float* l, int idx) {
-      u64 w[kVec], s = 0;
+  if (warp < kIts) {
+    before = sh.found_sum + incl - s;
+    for (int i = 0; i < warp; ++i) before += sh.scan[i];
+    if (before < target && before + s >= target) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) { w[i] = weight(l[i], idx + i); s += w[i]; }
-      u64 incl = s;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const u64 x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
-      u64 at = before + incl - s;
-      if (at < target && at + s >= target) {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) { if (at < target && at + w[i] >= target) token = idx + i; at += w[i]; }
-      }
-      before += __shfl_sync(0xffffffffu, incl, 31);
-    });
+      for (int i = 0; i < kVec; ++i) { if (before < target && before + w[i] >= target) token = idx + i; before += w[i]; }
+    }
   }
   return token;
 }
@@ -576,6 +641,10 @@ struct CatBound {
   int idx;
   __device__ __forceinline__ bool kept(float t, int i) const { return t > value || (t == value && i <= idx); }
 };
+// Adds in shared memory where p < limit, without a branch.
+__device__ __forceinline__ void cat_add_if(uint32_t* at, uint32_t v, uint32_t p, uint32_t limit) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.lt.u32 p, %2, %3;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(smem_u32(at)), "r"(v), "r"(p), "r"(limit) : "memory");
+}
 // Distance from the largest in units of 1/64, kCatFrac bits behind the point; kCatBins and more: below every bin (masked too).
 __device__ __forceinline__ uint32_t cat_place(float m, float l, float inv_t) {
   return __float2uint_rd(fminf((m - __fmul_rn(l, inv_t)) * (kCatPerUnit * (1 << kCatFrac)), 4095.0f * (1 << kCatFrac)));
@@ -760,9 +829,14 @@ __device__ __forceinline__ void cat_finish(CatShared& sh, const CatParams& p, in
       if (before < target && before + own >= target) found = static_cast<int>(idx);
     }
   } else {
-    found = cat_locate(sh, row, seg, target, kept.listed, [&](u64 key) { return cat_weight(cat_key_value(key), sc, sh.tab); }, [&](float l, int idx) -> u64 {
-      const float t = cat_scale(l, inv_t);
-      return bound.kept(t, idx) ? cat_weight(t, sc, sh.tab) : 0;
+    found = cat_locate(sh, row, seg, target, kept.listed, [&](u64 key) { return cat_weight(cat_key_value(key), sc, sh.tab); },
+                       [&](const float* l, int idx, u64* w) {
+#pragma unroll
+      for (int i = 0; i < CatRow<T>::kVec; ++i) {
+        const float t = cat_scale(l[i], inv_t);
+        const u64 x = cat_weight(t, sc, sh.tab);
+        w[i] = bound.kept(t, idx + i) ? x : 0;
+      }
     });
   }
   if (found >= 0) {
@@ -847,12 +921,14 @@ __global__ void __launch_bounds__(kCatThreads) cat_top_kernel(const __grid_const
   const uint32_t own = cat_ord(mine);
   uint32_t tau = 0;
   if (q.few) {
-    const int share = (q.want + p.w.splits - 1) / p.w.splits;
+    // its share goes by its part of the row (the last one's may be short)
+    const int mine_n = min(p.w.share * kCatPiece, max(p.V + row.head - split * p.w.share * kCatPiece, 0));
+    const int share = static_cast<int>((static_cast<int64_t>(q.want) * mine_n + p.V - 1) / p.V);
     uint32_t lo = 0, hi = 0xff800000u;   // fewer than share at lo (none are that large), share at hi (if at all)
     while (hi - lo > 1) {
       const uint32_t at = lo + (hi - lo) / 2;
       const int n = __syncthreads_count(own <= at);
-      if (n >= share) { hi = at; if (n <= share + share / 4 + 2) break; } else lo = at;
+      if (n >= share) { hi = at; if (n <= share + share / 16) break; } else lo = at;
     }
     tau = hi;
   }
@@ -1045,10 +1121,10 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
 #pragma unroll
       for (int i = 0; i < kVec; ++i) at[i] = cat_place(m, l[i], q.inv_t);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) if (at[i] < (kCatBins << kCatFrac)) atomicAdd(&sh.hist[at[i] >> kCatFrac], 1u);
+      for (int i = 0; i < kVec; ++i) cat_add_if(sh.hist + (at[i] >> kCatFrac), 1u, at[i], kCatBins << kCatFrac);
       if (q.by_p) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) if (at[i] < (kCatBins << kCatFrac)) atomicAdd(&sh.hist[kCatBins + (at[i] >> kCatFrac)], at[i] & ((1u << kCatFrac) - 1));
+        for (int i = 0; i < kVec; ++i) cat_add_if(sh.hist + kCatBins + (at[i] >> kCatFrac), at[i] & ((1u << kCatFrac) - 1), at[i], kCatBins << kCatFrac);
       }
     });
     __syncthreads();
@@ -1315,15 +1391,17 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
     __threadfence();
   }
   if (total == 0) return;
-  const int found = cat_locate(sh, row, seg, cat_target(p.w[b], total), 0, [](u64) -> u64 { return 0; }, [&](float l, int idx) -> u64 {
-    const float t = cat_scale(l, inv_p);
-    if (!kept_p.kept(t, idx)) return 0;
-    double a = sp.exp(t, sh.tab);
-    if (minus) {
-      const float tq = cat_scale(cat_float(qrow.base[qrow.head + idx]), inv_q);
-      if (kept_q.kept(tq, idx)) a -= sq.exp(tq, sh.tab);
+  const int found = cat_locate(sh, row, seg, cat_target(p.w[b], total), 0, [](u64) -> u64 { return 0; }, [&](const float* l, int idx, u64* w) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      const float t = cat_scale(l[i], inv_p);
+      double a = kept_p.kept(t, idx + i) ? sp.exp(t, sh.tab) : 0.0;
+      if (minus && a > 0.0) {
+        const float tq = cat_scale(cat_float(qrow.base[qrow.head + idx + i]), inv_q);
+        if (kept_q.kept(tq, idx + i)) a -= sq.exp(tq, sh.tab);
+      }
+      w[i] = static_cast<u64>(__double_as_longlong(fmax(a, 0.0) + 1.0) - 0x3ff0000000000000ll);
     }
-    return static_cast<u64>(__double_as_longlong(fmax(a, 0.0) + 1.0) - 0x3ff0000000000000ll);
   });
   if (found >= 0) p.x_new[b] = found;
 }
