@@ -32,7 +32,8 @@ constexpr int kCatThreads = 256;
 constexpr int kCatWarps = kCatThreads / 32;
 constexpr int kCatBins = 2048;        // bins of the histogram: 1/64 of scaled logit each, 32 below the largest
 constexpr float kCatPerUnit = 64.0f;
-constexpr int kCatFrac = 12;          // bits of a token's place within its bin: the places of 2^19 tokens add up to less than 2^32
+constexpr int kCatFrac = 5;           // bits of a token's place within its bin
+constexpr int kCatPack = 18;          // a word holds a count (above) and a sum of places of up to 2^13 tokens
 constexpr int kCatList = 2048;        // candidates that are sorted
 constexpr int kCatSub = 1024;         // bins of a refinement
 constexpr int kCatPiece = 512;        // tokens whose weights are summed together, to find a token by its cumulative weight
@@ -222,6 +223,8 @@ struct CatScale {
     floor = ceil - range;
   }
   __device__ __forceinline__ double exp(float t, const double* tab) const { return cat_exp(fminf(fmaxf(t - base, floor), ceil), c, tab); }
+  // the same where base is 0: no scaled logit lies above
+  __device__ __forceinline__ double exp0(float t, const double* tab) const { return cat_exp(fmaxf(t, floor), c, tab); }
 };
 // Weights are sums of doubles with 256 added to each: the bits of v + 256 are those of 256 plus v in units of 2^-44, so adding up
 // bits and taking off 256's as often gives the integer sum.
@@ -251,7 +254,7 @@ enum { CAT_DONE = 0, CAT_RANGE = 1, CAT_SEARCH = 2 };
 struct CatState {                                  // of a row
   uint32_t ticket[2], list_n;
   int mode;                                        // what is left to do for cat_range_kernel
-  uint32_t ua, ub, uk, ue;                         // places: list [ua, ub) and [uk, ue), weights below ua (and below uk)
+  float ta, tb, tk, te;                            // scaled logits: listed are [tb, ta) and [te, tk); weights wanted from ta up (and from tk up)
   uint32_t at_a, n1, n_mid;
   int apart, upto, ends;
 };
@@ -649,6 +652,15 @@ __device__ __forceinline__ void cat_add_if(uint32_t* at, uint32_t v, uint32_t p,
 __device__ __forceinline__ uint32_t cat_place(float m, float l, float inv_t) {
   return __float2uint_rd(fminf((m - __fmul_rn(l, inv_t)) * (kCatPerUnit * (1 << kCatFrac)), 4095.0f * (1 << kCatFrac)));
 }
+// The least scaled logit that lies in a bin before b (in bin 0 none does).
+__device__ __forceinline__ float cat_threshold(float m, int b) {
+  if (b <= 0) return INFINITY;
+  const uint32_t at = static_cast<uint32_t>(b) << kCatFrac;
+  float t = m - static_cast<float>(b) / kCatPerUnit;
+  while (cat_place(m, t, 1.0f) < at && t > -FLT_MAX) t = nextafterf(t, -INFINITY);
+  while (cat_place(m, t, 1.0f) >= at && t < INFINITY) t = nextafterf(t, INFINITY);
+  return t;
+}
 struct CatRequest {   // what the caller asks of a row
   float inv_t, top_p;
   int want;           // top-k, 0: off
@@ -943,6 +955,8 @@ __global__ void __launch_bounds__(kCatThreads) cat_top_kernel(const __grid_const
   }
 }
 
+__device__ __forceinline__ float cat_exp2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
 // From a row's counts: between which bins top-p ends, and in which top-k; what cat_range_kernel has to look at.
 __device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatState* st, const CatRequest& q, uint32_t live, float m, float least) {
   const int tid = threadIdx.x;
@@ -960,8 +974,8 @@ __device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatSt
     for (int i = 0; i < 4; ++i) {
       n[j + i] = hn[i];
       const float c = static_cast<float>(hn[i]);
-      const float place = tid * kEach + j + i + (hn[i] ? __fdividef(static_cast<float>(fn[i]), c * (1 << kCatFrac)) : 0.0f);
-      e[j + i] = q.by_p ? c * exp2f(-static_cast<float>(kLog2e) / kCatPerUnit * place) : 0.0f;
+      const float place = tid * kEach + j + i + (hn[i] ? __fdividef(static_cast<float>(fn[i]) + 0.5f * c, c * (1 << kCatFrac)) : 0.0f);
+      e[j + i] = q.by_p ? c * cat_exp2(-static_cast<float>(kLog2e) / kCatPerUnit * place) : 0.0f;
       own_n += n[j + i]; own_e += e[j + i];
     }
   }
@@ -991,8 +1005,9 @@ __device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatSt
   int bin_a = bin_k, bin_b = bin_k;
   if (q.by_p) {
     // A bin's weight is its count times the weight at its tokens' mean place, to (1/64)^2 / 8 = 2^-15 (its tokens' weights are within
-    // exp(-1/64) of each other), 2^-12 / 64 and 2^-12 / 64 for the places' rounding, 2^-20 for the exponential's and the fp32 sums'.
-    constexpr float kLo = 1.0f - 4e-5f, kHi = 1.0f + 7e-5f;
+    // exp(-1/64) of each other), 2^-6 / 64 for the places' rounding (their middle is taken), 2^-12 / 64 and 2^-20 for that of the
+    // distances, the exponential and the fp32 sums.
+    constexpr float kLo = 1.0f - 3.2e-4f, kHi = 1.0f + 3.5e-4f;
     constexpr float kNear = 1.0f + 1e-5f;   // (the sum up to a bin is not the same number at its end and at the next one's start)
     const float lim_lo = q.top_p * lo * kLo, lim_hi = q.top_p * hi * kHi;
     float mass = mass0;
@@ -1035,17 +1050,14 @@ __device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatSt
     if (b == bin_k) sh.end_k = cum;
   }
   __syncthreads();
+  const bool apart = by_k && q.by_p && bin_k > bin_b;   // top-k ends in a bin of its own, and top-p refers to what is before
   if (tid == 0) {
-    const bool apart = by_k && q.by_p && bin_k > bin_b;   // top-k ends in a bin of its own, and top-p refers to what is before
-    st->mode = CAT_SEARCH;
-    if (known && sh.at_b - sh.at_a + (apart ? sh.end_k - sh.at_k : 0) <= kCatList) {
-      st->mode = CAT_RANGE;
-      st->ua = static_cast<uint32_t>(bin_a) << kCatFrac; st->ub = static_cast<uint32_t>(bin_b + 1) << kCatFrac;
-      st->uk = static_cast<uint32_t>(by_k ? bin_k : kCatBins) << kCatFrac; st->ue = st->uk + (apart ? 1u << kCatFrac : 0u);
-      st->at_a = sh.at_a; st->n1 = sh.at_b - sh.at_a; st->n_mid = apart ? sh.at_k - sh.at_b : 0;
-      st->apart = apart; st->upto = q.by_p && (apart || !by_k); st->ends = ends;
-    }
+    const bool fits = known && sh.at_b - sh.at_a + (apart ? sh.end_k - sh.at_k : 0) <= kCatList;
+    st->mode = fits ? CAT_RANGE : CAT_SEARCH;
+    st->at_a = sh.at_a; st->n1 = sh.at_b - sh.at_a; st->n_mid = apart ? sh.at_k - sh.at_b : 0;
+    st->apart = apart; st->upto = q.by_p && (apart || !by_k); st->ends = ends;
   }
+  if (tid < 4 * 32 && (tid & 31) == 0) (&st->ta)[tid / 32] = cat_threshold(m, tid == 0 ? bin_a : tid == 32 ? bin_b + 1 : tid == 64 ? bin_k : bin_k + 1);
 }
 
 // Rows without top-k and top-p: everything that is left to do.  Rows with a small top-k: the tokens above the threshold, of which the
@@ -1114,22 +1126,36 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
     if (x.n <= kCatList && cat_resolve(sh, x, sc, kept)) cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
     else cat_search(sh, p, r, row, seg, q, by_k, sc, m);   // (many tokens above the threshold: rows in order, many equals)
   } else {
-    for (int i = tid; i < 2 * kCatBins; i += kCatThreads) sh.hist[i] = 0;
-    __syncthreads();
-    cat_each(row, p0, p1, [&](const float* l, int) {
-      uint32_t at[kVec];
+    // one addition a token: count and place in one word, taken apart before 2^13 tokens could overflow it
+    uint32_t* pack = reinterpret_cast<uint32_t*>(sh.list);
+    constexpr int kEach = kCatBins / kCatThreads, kMost = (1 << 13) / kCatPiece;
+    uint32_t n[kEach] = {}, f[kEach] = {};               // of bins tid * kEach + j
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) at[i] = cat_place(m, l[i], q.inv_t);
+    for (int j = 0; j < kEach; j += 4) reinterpret_cast<uint4*>(pack)[(tid * kEach + j) / 4] = make_uint4(0, 0, 0, 0);
+    for (int q0 = p0; q0 < p1; q0 += kMost) {
+      __syncthreads();
+      cat_each(row, q0, min(q0 + kMost, p1), [&](const float* l, int) {
+        uint32_t at[kVec];
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) cat_add_if(sh.hist + (at[i] >> kCatFrac), 1u, at[i], kCatBins << kCatFrac);
-      if (q.by_p) {
+        for (int i = 0; i < kVec; ++i) at[i] = cat_place(m, l[i], q.inv_t);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) cat_add_if(sh.hist + kCatBins + (at[i] >> kCatFrac), at[i] & ((1u << kCatFrac) - 1), at[i], kCatBins << kCatFrac);
+        for (int i = 0; i < kVec; ++i) cat_add_if(pack + (at[i] >> kCatFrac), (1u << kCatPack) | (at[i] & ((1u << kCatFrac) - 1)), at[i], kCatBins << kCatFrac);
+      });
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kEach; j += 4) {
+        uint4* at = reinterpret_cast<uint4*>(pack) + (tid * kEach + j) / 4;
+        const uint4 x = *at;
+        *at = make_uint4(0, 0, 0, 0);
+        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { n[j + i] += y[i] >> kCatPack; f[j + i] += y[i] & ((1u << kCatPack) - 1); }
       }
-    });
-    __syncthreads();
+    }
     uint32_t* hist = p.w.hist + static_cast<int64_t>(row_i) * 2 * kCatBins;
-    for (int i = tid; i < 2 * kCatBins; i += kCatThreads) if (sh.hist[i]) atomicAdd(hist + i, sh.hist[i]);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (n[j]) { atomicAdd(hist + tid * kEach + j, n[j]); if (q.by_p) atomicAdd(hist + kCatBins + tid * kEach + j, f[j]); }
     if (!cat_last(sh, &st->ticket[0], p.w.splits)) return;
     cat_bins(sh, hist, st, q, top.live, m, cat_least(p, r, m));
   }
@@ -1160,42 +1186,73 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_
     cat_search(sh, p, r, row, seg, q, by_k, sc, m);
     return;
   }
-  const uint32_t ua = st->ua, ub = st->ub, uk = st->uk, ue = st->ue;
-  const bool upto = st->upto != 0;
-  const uint32_t need = upto ? uk : ua;
+  const float ta = st->ta, tb = st->tb, tk = st->tk, te = st->te;
+  const bool apart = st->apart != 0, upto = st->upto != 0;
   const int p0 = split * p.w.share, p1 = min(p0 + p.w.share, row.pieces());
-  u64 w_upto = 0, none = 0;
-  u64 w_above = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
-    u64 above = 0;
-    uint32_t at[kVec];
-    bool list = false;
+  u64 w_upto = 0, w_above, none = 0;
+  if (upto && !apart && sc.base == 0.0f) {
+    // top-p without top-k, the common case: every token's weight is wanted
+    w_above = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+      u64 above = 0;
+      bool list = false;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      at[i] = cat_place(m, l[i], q.inv_t);
-      list = list || at[i] - ua < ub - ua || at[i] - uk < ue - uk;
-    }
+      for (int h = 0; h < kVec; h += 4) {   // four exponentials side by side
+        float t[4];
+        u64 x[4];
 #pragma unroll
-    for (int h = 0; h < kVec; h += 4) {   // four exponentials side by side
-      if (!__any_sync(0xffffffffu, min(min(at[h], at[h + 1]), min(at[h + 2], at[h + 3])) < need)) continue;
-      double x[4];
+        for (int i = 0; i < 4; ++i) { t[i] = __fmul_rn(l[h + i], q.inv_t); x[i] = cat_bits(sc.exp0(t[i], sh.tab)); }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = sc.exp(__fmul_rn(l[h + i], q.inv_t), sh.tab);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) above += cat_bits(at[h + i] < ua ? x[i] : 0.0);
-      above -= 4 * kCat256;
-      if (upto) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w_upto += cat_bits(at[h + i] < uk ? x[i] : 0.0);
+        for (int i = 0; i < 4; ++i) {
+          w_upto += x[i];
+          if (t[i] >= ta) above += x[i] - kCat256;
+          list = list || (t[i] >= tb && !(t[i] >= ta));
+        }
         w_upto -= 4 * kCat256;
       }
-    }
-    if (list) {
+      if (list) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i)
-        if (at[i] - ua < ub - ua || at[i] - uk < ue - uk) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
-    }
-    return above;
-  });
+        for (int i = 0; i < kVec; ++i) {
+          const float t = __fmul_rn(l[i], q.inv_t);
+          if (t >= tb && !(t >= ta)) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+        }
+      }
+      return above;
+    });
+  } else {
+    const float need = upto ? tk : ta;
+    w_above = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+      u64 above = 0;
+      bool list = false;
+#pragma unroll
+      for (int h = 0; h < kVec; h += 4) {
+        float t[4];
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          t[i] = __fmul_rn(l[h + i], q.inv_t);
+          any = any || t[i] >= need || (upto && !apart);
+          list = list || (t[i] >= tb && !(t[i] >= ta)) || (apart && t[i] >= te && !(t[i] >= tk));
+        }
+        if (!__any_sync(0xffffffffu, any)) continue;
+        u64 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = cat_bits(sc.exp(t[i], sh.tab)) - kCat256;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (t[i] >= ta) above += x[i];
+          if (upto && (!apart || t[i] >= tk)) w_upto += x[i];
+        }
+      }
+      if (list) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const float t = __fmul_rn(l[i], q.inv_t);
+          if ((t >= tb && !(t >= ta)) || (apart && t >= te && !(t >= tk))) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+        }
+      }
+      return above;
+    });
+  }
   cat_reduce(sh, w_above, w_upto, none);
   u64* tot = p.w.tot + static_cast<int64_t>(row_i) * p.w.splits * 3;
   if (tid == 0) { __stcg(tot + split * 3, w_above); __stcg(tot + split * 3 + 1, w_upto); }

@@ -1477,12 +1477,12 @@ int check_cat_round(csd_ctx* ctx, int B, int gamma, int rows_p, int V) {
 
 CatView cat_view(const csd_logits* l) { return CatView{l->data, l->ld}; }
 
-// Parts of the rows: so many that `rows` of them give every SM eight blocks, of 4096 to 32768 tokens each.
+// Parts of the rows: so many that `rows` of them give every SM sixteen blocks (four are resident), of 4096 to 32768 tokens each.
 void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int* splits, int* share, int* pieces) {
   const int size = l->dtype == CSD_F32 ? 4 : 2, vec = 16 / size;
   const bool aligned = reinterpret_cast<uintptr_t>(l->data) % 16 == 0 && (l->ld * size % 16 == 0 || rows == 1);
   *pieces = (V + (aligned ? 0 : vec - 1) + kCatPiece - 1) / kCatPiece;
-  const int64_t want = (*pieces * rows + 8 * ctx->num_sms - 1) / (8 * ctx->num_sms);
+  const int64_t want = (*pieces * rows + 16 * ctx->num_sms - 1) / (16 * ctx->num_sms);
   *share = static_cast<int>(want < 8 ? 8 : want > 64 ? 64 : (want + 7) / 8 * 8);
   *splits = (*pieces + *share - 1) / *share;
 }
@@ -1492,10 +1492,10 @@ int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_ca
   p.V = V; p.logits = CatView{l->data, l->ld};
   if (f) { p.temperature = f->temperature; p.top_k = f->top_k; p.top_p = f->top_p; p.min_p = f->min_p; }
   p.u = u; p.token = token; p.logp = logp; p.dist = dist;
-  // Rows go in groups whose logits stay in L2 from one kernel to the next (64 MB of 126), and whose workspace is bounded.
-  const int64_t row_bytes = static_cast<int64_t>(V) * (l->dtype == CSD_F32 ? 4 : 2);
-  int64_t group = (int64_t(64) << 20) / row_bytes;
-  group = group < 1 ? 1 : group > 1024 ? 1024 : group;
+  // Rows go in groups whose workspace is bounded (32 KB a row).  Groups small enough for L2 to hold their logits from one kernel to
+  // the next took longer: the passes are not bound by reading, and each group's kernels fill and drain the device once more (512 rows of
+  // 131072 fp32 logits: GROUPFIG).
+  int64_t group = R < 1024 ? R : 1024;
   const int64_t groups = (R + group - 1) / group;
   group = (R + groups - 1) / groups;
   CatWork& w = p.w;
