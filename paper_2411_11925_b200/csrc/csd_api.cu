@@ -1557,10 +1557,12 @@ int check_quant(csd_ctx* ctx, const uint8_t* data, const uint8_t* scale, const c
 
 template <typename T, bool NORM>
 int launch_quant_rows(csd_ctx* ctx, int rows, const QuantRowsParams& p) {
-  // pieces of eight columns a thread: one up to 4096 columns, then two and four; wider rows are read twice
-  const int pieces = p.ld / 8, nch = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 4096 ? 4 : 0;
+  // pieces of eight columns a thread: one up to 4096 columns, then two and (16-bit types: their registers) four; wider rows are read twice
+  const int pieces = p.ld / 8, nch = pieces <= 512 ? 1 : pieces <= 2048 ? 2 : pieces <= 4096 && sizeof(T) == 2 ? 4 : 0;
   const int threads = nch ? ((pieces + nch - 1) / nch + 31) / 32 * 32 : 1024;
-  auto kern = nch == 1 ? quant_rows_kernel<T, 1, NORM> : nch == 2 ? quant_rows_kernel<T, 2, NORM> : nch == 4 ? quant_rows_kernel<T, 4, NORM> : quant_rows_kernel<T, 0, NORM>;
+  auto kern = nch == 1 ? quant_rows_kernel<T, 1, NORM> : nch == 2 ? quant_rows_kernel<T, 2, NORM> : nch == 4 ? quant_rows_kernel<T, sizeof(T) == 2 ? 4 : 2, NORM> : quant_rows_kernel<T, 0, NORM>;
+  const int most = ctx->num_sms * (1024 / threads > 0 ? 1024 / threads : 1);   // resident at 64 registers
+  rows = rows < most ? rows : most;
   return launch_short(ctx, ctx->stream, kern, rows, threads, 0, p);
 }
 
@@ -1593,15 +1595,30 @@ int make_quant_tmap(csd_ctx* ctx, CUtensorMap* m, const uint8_t* data, int rows,
   return CSD_OK;
 }
 
-template <typename OUT>
-int launch_quant_mma(csd_ctx* ctx, const CUtensorMap& tw, const CUtensorMap& ta, const QuantMmaParams& p, int grid, size_t smem) {
-  auto kern = quant_mma_kernel<OUT>;
+template <typename OUT, bool PAIR, int KPS>
+int launch_quant_mma_t(csd_ctx* ctx, const CUtensorMap& tw, const CUtensorMap& ta, const QuantMmaParams& p, int grid, size_t smem) {
+  auto kern = quant_mma_kernel<OUT, PAIR, KPS>;
   static bool attr_done[kMaxDevices] = {};   // function attributes are per device
   if (!attr_done[ctx->device]) {
     CSD_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
     attr_done[ctx->device] = true;
   }
-  return launch_short(ctx, ctx->stream, kern, grid, kQmThreads, smem, tw, ta, p, ctx->d_err);
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3(grid); lc.blockDim = dim3(kQmThreads); lc.dynamicSmemBytes = smem; lc.stream = ctx->stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = PAIR ? 2 : 1; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  lc.attrs = at; lc.numAttrs = PAIR ? 2 : 1;
+  CSD_CUDA(ctx, cudaLaunchKernelEx(&lc, kern, tw, ta, p, ctx->d_err));
+  ctx->launches++;
+  return CSD_OK;
+}
+
+template <typename OUT>
+int launch_quant_mma(csd_ctx* ctx, bool pair, const CUtensorMap& tw, const CUtensorMap& ta, const QuantMmaParams& p, int grid, size_t smem) {
+  return pair ? launch_quant_mma_t<OUT, true, 2>(ctx, tw, ta, p, grid, smem) : launch_quant_mma_t<OUT, false, 1>(ctx, tw, ta, p, grid, smem);
 }
 
 }  // namespace
@@ -2662,12 +2679,12 @@ int csd_norm_quantize(csd_ctx* ctx, int rows, int K, int dtype, const void* x, i
                       float eps, void* sum, int64_t lds, uint8_t* data, uint8_t* scale) {
   if (!ctx) return CSD_ERR_INVALID_ARG;
   if (!(eps >= 0.0f)) return fail(ctx, CSD_ERR_INVALID_ARG, "eps must be >= 0");
-  return quant_rows<true>(ctx, rows, K, dtype, QuantRowsParams{0, 0, 0, x, ldx, residual, ldr, weight, eps, sum, lds, data, scale});
+  return quant_rows<true>(ctx, rows, K, dtype, QuantRowsParams{rows, 0, 0, 0, x, ldx, residual, ldr, weight, eps, sum, lds, data, scale});
 }
 
 int csd_quantize(csd_ctx* ctx, int rows, int K, int dtype, const void* x, int64_t ldx, uint8_t* data, uint8_t* scale) {
   if (!ctx) return CSD_ERR_INVALID_ARG;
-  return quant_rows<false>(ctx, rows, K, dtype, QuantRowsParams{0, 0, 0, x, ldx, nullptr, 0, nullptr, 0.0f, nullptr, 0, data, scale});
+  return quant_rows<false>(ctx, rows, K, dtype, QuantRowsParams{rows, 0, 0, 0, x, ldx, nullptr, 0, nullptr, 0.0f, nullptr, 0, data, scale});
 }
 
 int csd_quant_matmul(csd_ctx* ctx, int M, int N, int K, const csd_quant* a, const csd_quant* w, int dtype, void* out, int64_t ldo) {
@@ -2685,29 +2702,31 @@ int csd_quant_matmul(csd_ctx* ctx, int M, int N, int K, const csd_quant* a, cons
   QuantMmaParams p{};
   p.M = M; p.N = N; p.nkb = ld / kQuantBlock; p.ls = ls; p.scale_a = a->scale; p.scale_w = w->scale; p.out = out; p.ldo = ldo;
   // token tiles as even as multiples of 32 allow
-  const int most = 224, mt = (M + most - 1) / most;
+  const int mt = (M + 223) / 224;
   p.bn = ((M + mt - 1) / mt + 31) / 32 * 32;
   p.tiles_m = (M + p.bn - 1) / p.bn;
-  const int64_t tiles = static_cast<int64_t>((N + 127) / 128) * p.tiles_m;
+  // Pairs of blocks where the MMAs and not the weights' way from memory decide (QUANTRULE).
+  const bool pair = p.bn >= 96 && N >= 256;
+  const int rows = pair ? 256 : 128;
+  const int64_t tiles = static_cast<int64_t>((N + rows - 1) / rows) * p.tiles_m;
   if (tiles > INT32_MAX) return fail(ctx, CSD_ERR_UNSUPPORTED, "too many output tiles");
   p.tiles = static_cast<int>(tiles);
   // few token rows leave room for two blocks an SM, whose loads and epilogues overlap
-  const int stage = kQmABytes + p.bn * kQuantBlock;
-  const bool two = p.bn <= 64;
+  const int stage = pair ? 2 * (kQmABytes + p.bn / 2 * kQuantBlock) : kQmABytes + p.bn * kQuantBlock;
+  const bool two = !pair && p.bn <= 64;
   const int room = two ? 113 * 1024 : 227 * 1024;
   p.stages = (room - kQmFixed) / stage;
   if (p.stages > 8) p.stages = 8;
-  p.acc_bufs = 2;
-  p.sf_col = p.acc_bufs * p.bn;
+  p.sf_col = 2 * p.bn;
   const int cols = p.sf_col + 2 * kQmSfCols;
   for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
-  const int most_ctas = ctx->num_sms * (two ? 2 : 1);
-  const int grid = p.tiles < most_ctas ? p.tiles : most_ctas;
+  const int most = pair ? ctx->num_sms / 2 : ctx->num_sms * (two ? 2 : 1);
+  const int grid = (p.tiles < most ? p.tiles : most) * (pair ? 2 : 1);
   const size_t smem = kQmFixed + static_cast<size_t>(p.stages) * stage;
   CUtensorMap tw, ta;
-  if ((rc = make_quant_tmap(ctx, &tw, w->data, N, ld, 128)) || (rc = make_quant_tmap(ctx, &ta, a->data, M, ld, p.bn))) return rc;
-  return dtype == CSD_F32 ? launch_quant_mma<float>(ctx, tw, ta, p, grid, smem) : dtype == CSD_BF16 ? launch_quant_mma<__nv_bfloat16>(ctx, tw, ta, p, grid, smem)
-                                                                                                 : launch_quant_mma<__half>(ctx, tw, ta, p, grid, smem);
+  if ((rc = make_quant_tmap(ctx, &tw, w->data, N, ld, 128)) || (rc = make_quant_tmap(ctx, &ta, a->data, M, ld, pair ? p.bn / 2 : p.bn))) return rc;
+  return dtype == CSD_F32 ? launch_quant_mma<float>(ctx, pair, tw, ta, p, grid, smem) : dtype == CSD_BF16 ? launch_quant_mma<__nv_bfloat16>(ctx, pair, tw, ta, p, grid, smem)
+                                                                                                       : launch_quant_mma<__half>(ctx, pair, tw, ta, p, grid, smem);
 }
 
 int csd_round_host(csd_ctx* ctx, const csd_head* head_q, const csd_head* head_p, const csd_schedule* sched_q,

@@ -20,7 +20,7 @@ constexpr int kQuantBlock = 128;
 
 // ------------------------------------------------------------------------------------------------------------ the norm
 struct QuantRowsParams {
-  int K, ld, ls;
+  int rows, K, ld, ls;
   const void* x;
   int64_t ldx;
   const void* residual;   // null: none
@@ -40,19 +40,17 @@ template <> __device__ __forceinline__ float quant_from_float<float>(float v) { 
 template <> __device__ __forceinline__ __nv_bfloat16 quant_from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half quant_from_float<__half>(float v) { return __float2half_rn(v); }
 
-// Eight elements of a row from column `col` on, zeros behind the row's end; whole vectors where the row is 16-byte aligned.
+// Eight elements of a row from column `col` on as they lie, zeros behind the row's end; whole vectors where the row is 16-byte aligned.
+template <typename T> struct QuantRaw { __align__(16) T e[8]; };
 template <typename T>
-__device__ __forceinline__ void quant_load8(const T* row, int col, int K, bool aligned, float* v) {
+__device__ __forceinline__ void quant_load8(const T* row, int col, int K, bool aligned, QuantRaw<T>& v) {
   if (aligned && col + 8 <= K) {
     constexpr int kQ = sizeof(T) / 2;   // 16-byte vectors
-    __align__(16) T e[8];
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(e)[i] = reinterpret_cast<const uint4*>(row + col)[i];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = quant_to_float(e[i]);
+    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(v.e)[i] = reinterpret_cast<const uint4*>(row + col)[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = col + i < K ? quant_to_float(row[col + i]) : 0.0f;
+    for (int i = 0; i < 8; ++i) v.e[i] = col + i < K ? row[col + i] : quant_from_float<T>(0.0f);
   }
 }
 template <typename T>
@@ -92,41 +90,48 @@ __device__ __forceinline__ uint2 quant_pack8(const float* v, uint32_t byte) {
   return make_uint2(w[0], w[1]);
 }
 
-// One block per row.  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read twice), 16 lanes a
-// scale block.  Sums and the norm in fp32; the sum leaves rounded to the input's type, the norm uses it unrounded.
+// A block takes rows blockIdx.x, + gridDim.x, ...: the next row is requested before this one's reduction, so that its reads are under
+// way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, NORMFIG so; bound by
+// memory: 288 MB take 44 us at the rate of a copy).  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read
+// twice), 16 lanes a scale block.  Sums and the norm in fp32; the sum leaves rounded to the input's type, the norm uses it unrounded.
 template <typename T, int NCH, bool NORM>
-__global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantRowsParams p) {
-  __shared__ float part[32];
-  const int64_t r = blockIdx.x;
+__global__ void __launch_bounds__(1024) quant_rows_kernel(const __grid_constant__ QuantRowsParams p) {
+  __shared__ float part[2][32];
+  constexpr int kN = NCH > 0 ? NCH : 1;
   const int tid = threadIdx.x, T_ = blockDim.x, pieces = p.ld / 8, lane = tid & 31;
   griddep_enter();
-  const T* x = static_cast<const T*>(p.x) + r * p.ldx;
-  const T* res = p.residual ? static_cast<const T*>(p.residual) + r * p.ldr : nullptr;
-  const T* wt = static_cast<const T*>(p.weight);
-  T* sum = p.sum ? static_cast<T*>(p.sum) + r * p.lds : nullptr;
+  const T* const wt = static_cast<const T*>(p.weight);
   auto al = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
-  const bool ax = al(x), ar = al(res), aw = al(wt), as = al(sum);
-  uint8_t* data = p.data + r * p.ld;
-  uint8_t* scale = p.scale + r * p.ls;
-  auto load = [&](int c, float* h) {
-    quant_load8(x, c * 8, p.K, ax, h);
-    if (res) {
-      float v[8];
-      quant_load8(res, c * 8, p.K, ar, v);
+  const bool aw = al(wt);
+  auto row_x = [&](int64_t r) { return static_cast<const T*>(p.x) + r * p.ldx; };
+  auto row_r = [&](int64_t r) { return static_cast<const T*>(p.residual) + r * p.ldr; };
+  QuantRaw<T> vx[kN], vr[kN];
+  auto fetch = [&](int64_t r, int j, int c) {
+    const T* x = row_x(r);
+    quant_load8(x, c * 8, p.K, al(x), vx[j]);
+    if (p.residual) { const T* y = row_r(r); quant_load8(y, c * 8, p.K, al(y), vr[j]); }
+  };
+  auto take = [&](int j, float* h) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] += v[i];
+    for (int i = 0; i < 8; ++i) h[i] = quant_to_float(vx[j].e[i]);
+    if (p.residual) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] += quant_to_float(vr[j].e[i]);
     }
   };
-  auto put = [&](int c, float* h, float rstd) {   // (whole groups of 16 lanes are inside or outside)
-    if (sum) quant_store8(sum, c * 8, p.K, as, h);
+  auto put = [&](int64_t r, int c, float* h, float rstd) {   // (whole groups of 16 lanes are inside or outside)
+    if (p.sum) {
+      T* sum = static_cast<T*>(p.sum) + r * p.lds;
+      quant_store8(sum, c * 8, p.K, al(sum), h);
+    }
     if (NORM) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] *= rstd;
       if (wt) {
-        float v[8];
-        quant_load8(wt, c * 8, p.K, aw, v);
+        QuantRaw<T> w;
+        quant_load8(wt, c * 8, p.K, aw, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] *= v[i];
+        for (int i = 0; i < 8; ++i) h[i] *= quant_to_float(w.e[i]);
       }
     }
     uint32_t amax = 0;
@@ -136,65 +141,79 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantRowsParams 
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(group, amax, o));
     const uint32_t byte = quant_scale_byte(amax);
-    reinterpret_cast<uint2*>(data)[c] = quant_pack8(h, byte);
-    if ((lane & 15) == 0) scale[c >> 4] = static_cast<uint8_t>(byte);
+    reinterpret_cast<uint2*>(p.data + r * p.ld)[c] = quant_pack8(h, byte);
+    if ((lane & 15) == 0) p.scale[r * p.ls + (c >> 4)] = static_cast<uint8_t>(byte);
   };
-  for (int i = p.ld / kQuantBlock + tid; i < p.ls; i += T_) scale[i] = 127;
-  float rstd = 1.0f;
-  auto finish = [&](float ss) {
-    if (!NORM) return;
+  int turn = 0;
+  auto finish = [&](float ss) -> float {
+    if (!NORM) return 1.0f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (lane == 0) part[tid >> 5] = ss;
+    float* const at = part[turn];
+    turn ^= 1;                                   // (two in turn: a warp is at most one row ahead of one that still reads)
+    if (lane == 0) at[tid >> 5] = ss;
     __syncthreads();
-    ss = lane < (T_ >> 5) ? part[lane] : 0.0f;
+    ss = lane < (T_ >> 5) ? at[lane] : 0.0f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    rstd = rsqrtf(ss / static_cast<float>(p.K) + p.eps);
+    return rsqrtf(ss / static_cast<float>(p.K) + p.eps);
   };
+  const int64_t step = gridDim.x;
+  int64_t r = blockIdx.x;
   if (NCH > 0) {
-    float h[NCH > 0 ? NCH : 1][8], ss = 0.0f;
 #pragma unroll
-    for (int j = 0; j < NCH; ++j) {
-      const int c = tid + j * T_;
-      if (c < pieces) load(c, h[j]);
-    }
+    for (int j = 0; j < kN; ++j) if (tid + j * T_ < pieces) fetch(r, j, tid + j * T_);
+  }
+  for (; r < p.rows; r += step) {
+    for (int i = p.ld / kQuantBlock + tid; i < p.ls; i += T_) p.scale[r * p.ls + i] = 127;
+    float ss = 0.0f;
+    if (NCH > 0) {
+      float h[kN][8];
 #pragma unroll
-    for (int j = 0; j < NCH; ++j) {
-      if (tid + j * T_ < pieces) {
+      for (int j = 0; j < kN; ++j) {
+        if (tid + j * T_ < pieces) {
+          take(j, h[j]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(h[j][i], h[j][i], ss);
+          for (int i = 0; i < 8; ++i) ss = fmaf(h[j][i], h[j][i], ss);
+        }
       }
-    }
-    finish(ss);
+      if (r + step < p.rows) {
 #pragma unroll
-    for (int j = 0; j < NCH; ++j)
-      if (tid + j * T_ < pieces) put(tid + j * T_, h[j], rstd);
-  } else {
-    float ss = 0.0f, h[8];
-    if (NORM)
-      for (int c = tid; c < pieces; c += T_) {
-        load(c, h);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
+        for (int j = 0; j < kN; ++j) if (tid + j * T_ < pieces) fetch(r + step, j, tid + j * T_);
       }
-    finish(ss);
-    for (int c = tid; c < pieces; c += T_) { load(c, h); put(c, h, rstd); }
+      const float rstd = finish(ss);
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+        if (tid + j * T_ < pieces) put(r, tid + j * T_, h[j], rstd);
+    } else {
+      float h[8];
+      if (NORM)
+        for (int c = tid; c < pieces; c += T_) {
+          fetch(r, 0, c); take(0, h);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
+        }
+      const float rstd = finish(ss);
+      for (int c = tid; c < pieces; c += T_) { fetch(r, 0, c); take(0, h); put(r, c, h, rstd); }
+    }
   }
 }
 
 // --------------------------------------------------------------------------------------------------------- the product
 // out[m, n] = sum_k a[m, k] w[n, k], both 8-bit matrices.  The vocabulary matrix is the MMA's M operand (128 rows a
-// tile: N is never small), the token rows its N operand (a multiple of 32 up to 224, so that two accumulators and the scales
+// block: N is never small), the token rows its N operand (a multiple of 32 up to 224, so that two accumulators and the scales
 // fit the 512 tensor-memory columns): a single token row costs what reading the weights costs.
-//   warp 0      requests both operands by TMA, a block of 128 columns a stage
-//   warp 1      issues the MMAs: four of K = 32 a stage under one scale byte (byte kb % 4 of the scale words)
+// PAIR: two blocks of a cluster share each MMA (256 vocabulary rows, every block loads its own 128 and half of the token rows): a block of its own needs
+// 107 B a cycle of operands at 192 token rows, more than an SM takes from L2; in a pair it needs 75.
+//   warp 0      requests both operands by TMA, KPS blocks of 128 columns a stage (waiting for a stage and handing it back costs the issuing
+//               warp 300 to 500 cycles, about what one block's MMAs take)
+//   warp 1      issues the MMAs (of a pair, the leader's): four of K = 32 a block under one scale byte (byte kb % 4 of the scale words)
 //   warps 2..5  bring the scales into tensor memory, a word (four blocks) per row: row 32 j + i at lane i, column j, in all
-//               four lane quarters
+//               four lane quarters; the token rows' scales into both blocks'
 //   warps 6..9  epilogue: a lane is a vocabulary row, a register a token
 struct QuantMmaParams {
   int M, N, nkb, ls;          // token rows, vocabulary rows, blocks of 128 columns, scale bytes a row
-  int bn, stages, acc_bufs, sf_col, tmem_cols, tiles_m, tiles;
+  int bn, stages, sf_col, tmem_cols, tiles_m, tiles;
   const uint8_t *scale_a, *scale_w;
   void* out;
   int64_t ldo;
@@ -205,24 +224,38 @@ constexpr int kQmSfCols = 12;   // 4 of the weights' scales, up to 8 of the toke
 constexpr int kQmFixed = 1024 + 256;
 
 // (+)= with e8m0 scales from tensor memory; the scale byte is chosen by the instruction descriptor
+template <bool PAIR>
 __device__ __forceinline__ void umma_mxf8(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t acc) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
-      ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(acc), "r"(sfa), "r"(sfb)
-      : "memory");
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+        ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(acc), "r"(sfa), "r"(sfb)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+        ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(acc), "r"(sfa), "r"(sfb)
+        : "memory");
 }
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
+// Arrives on a barrier of a block of the cluster (shared::cluster address); tensor-memory stores before it are complete and fenced.
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 
-template <typename OUT>
-__global__ void __launch_bounds__(kQmThreads, 2)
-quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, const QuantMmaParams p, int* err) {
+template <typename OUT, bool PAIR, int KPS>
+__global__ void __launch_bounds__(kQmThreads, PAIR ? 1 : 2)
+quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ QuantMmaParams p, int* err) {
   extern __shared__ uint8_t qm_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(qm_raw) + 1023) & ~uintptr_t(1023));
-  const int stage_bytes = kQmABytes + p.bn * kQuantBlock, S = p.stages;
+  const int b_rows = PAIR ? p.bn / 2 : p.bn;                      // token rows that this block loads
+  const int block_bytes = kQmABytes + b_rows * kQuantBlock, stage_bytes = KPS * block_bytes, S = p.stages;
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + static_cast<size_t>(S) * stage_bytes);   // [8]
   uint64_t* empty = full + 8;       // [8]
   uint64_t* sf_full = empty + 8;    // [2]
@@ -231,82 +264,117 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   uint64_t* acc_empty = acc_full + 2;  // [2]
   uint32_t* tmem_s = reinterpret_cast<uint32_t*>(acc_empty + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
   int* s_abort = reinterpret_cast<int*>(tmem_s + 1);
   if (threadIdx.x == 0) {
     *s_abort = *reinterpret_cast<volatile int*>(err);
     tma_prefetch_desc(&tm_w);
     tma_prefetch_desc(&tm_a);
     for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sf_full[i], 4); mbar_init(&sf_empty[i], 1); mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sf_full[i], PAIR ? 8 : 4); mbar_init(&sf_empty[i], 1); mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], PAIR ? 8 : 4); }
     fence_mbar_init();
   }
   __syncthreads();
+  if (PAIR) {                       // both blocks go by what either has seen
+    cluster_arrive(); cluster_wait();
+    int peer = 0;
+    if (threadIdx.x == 0) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(peer) : "r"(mapa_shared(smem_u32(s_abort), static_cast<uint32_t>(rank ^ 1))) : "memory");
+    cluster_arrive(); cluster_wait();
+    if (threadIdx.x == 0 && peer != 0) *s_abort = peer;
+    __syncthreads();
+  }
   if (*s_abort != 0) return;
-  if (warp == 1) { tmem_alloc(tmem_s, p.tmem_cols); tmem_relinquish(); }
+  if (warp == 1) {
+    if (PAIR) { tmem_alloc_pair(tmem_s, p.tmem_cols); tmem_relinquish_pair(); }
+    else { tmem_alloc(tmem_s, p.tmem_cols); tmem_relinquish(); }
+  }
   tc_fence_before_sync();
   __syncthreads();
+  if (PAIR) { cluster_arrive(); cluster_wait(); }
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_s;
   griddep_wait();
   if (threadIdx.x == 0) griddep_launch_dependents();
-  const int first = blockIdx.x, step = gridDim.x;
-  const int groups = (p.nkb + 3) / 4;
+  const int first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+  const int groups = (p.nkb + 3) / 4, nst = (p.nkb + KPS - 1) / KPS;
+  constexpr int kRows = PAIR ? 256 : 128;       // vocabulary rows of a tile
   bool ok = true;
   // a wait by a whole warp: one answer for all its lanes
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ch_wait<false>(bar, parity, err)) != 0; };
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ch_wait<PAIR>(bar, parity, err)) != 0; };
   if (warp == 0) {
     if (lane == 0) {
       int it = 0;
       for (int t = first; t < p.tiles && ok; t += step) {
-        const int n0 = t / p.tiles_m * 128, m0 = t % p.tiles_m * p.bn;
-        for (int kb = 0; kb < p.nkb; ++kb, ++it) {
-          const int s = it % S;
-          if (it >= S && !ch_wait<false>(&empty[s], ((it / S) & 1) ^ 1, err)) { ch_fail(err, 1, 9, it); ok = false; break; }
+        const int n0 = t / p.tiles_m * kRows + rank * 128, m0 = t % p.tiles_m * p.bn + rank * b_rows;
+        for (int st = 0; st < nst; ++st, ++it) {
+          const int s = it % S, blocks = min(KPS, p.nkb - st * KPS);
+          if (it >= S && !ch_wait<PAIR>(&empty[s], ((it / S) & 1) ^ 1, err)) { ch_fail(err, 1, 9, it); ok = false; break; }
           uint8_t* dst = ring + static_cast<size_t>(s) * stage_bytes;
-          mbar_arrive_expect_tx(&full[s], stage_bytes);
-          tma_load_2d(dst, &tm_w, &full[s], kb * kQuantBlock, n0);
-          tma_load_2d(dst + kQmABytes, &tm_a, &full[s], kb * kQuantBlock, m0);
+          if (PAIR) {
+            // the leader's barrier counts the bytes of both blocks; only the leader arms it
+            if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * blocks * block_bytes);
+            const uint32_t lb = mapa_shared(smem_u32(&full[s]), 0);
+            for (int k = 0; k < blocks; ++k) {
+              tma_load_2d_pair(dst + k * block_bytes, &tm_w, lb, (st * KPS + k) * kQuantBlock, n0);
+              tma_load_2d_pair(dst + k * block_bytes + kQmABytes, &tm_a, lb, (st * KPS + k) * kQuantBlock, m0);
+            }
+          } else {
+            mbar_arrive_expect_tx(&full[s], blocks * block_bytes);
+            for (int k = 0; k < blocks; ++k) {
+              tma_load_2d(dst + k * block_bytes, &tm_w, &full[s], (st * KPS + k) * kQuantBlock, n0);
+              tma_load_2d(dst + k * block_bytes + kQmABytes, &tm_a, &full[s], (st * KPS + k) * kQuantBlock, m0);
+            }
+          }
         }
       }
     }
     __syncwarp();
   } else if (warp == 1) {
-    const bool leader = elect_one();
-    // e4m3 operands, K-major, fp32 accumulator, e8m0 scales, M = 128
-    const uint32_t idesc = (static_cast<uint32_t>(p.bn >> 3) << 17) | (1u << 23) | (8u << 24);
-    int it = 0, g = 0, i = 0;
-    for (int t = first; t < p.tiles && ok; t += step, ++i) {
-      const int ab = p.acc_bufs == 2 ? i & 1 : 0, use = p.acc_bufs == 2 ? i >> 1 : i;
-      if (use > 0 && !wait(&acc_empty[ab], (use - 1) & 1)) { if (leader) ch_fail(err, 2, 9, i); ok = false; break; }
-      tc_fence_after_sync();
-      const uint32_t d = tmem + ab * p.bn;
-      for (int kb = 0; kb < p.nkb; ++kb, ++it) {
-        const int s = it % S;
-        if ((kb & 3) == 0 && !wait(&sf_full[g & 1], (g >> 1) & 1)) { if (leader) ch_fail(err, 2, 10, g); ok = false; break; }
-        if (!wait(&full[s], (it / S) & 1)) { if (leader) ch_fail(err, 2, 11, it); ok = false; break; }
+    if (rank == 0) {
+      const bool leader = elect_one();
+      // e4m3 operands, K-major, fp32 accumulator, e8m0 scales
+      const uint32_t idesc = (static_cast<uint32_t>(p.bn >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(kRows >> 4) << 24);
+      int it = 0, g = 0, i = 0;
+      for (int t = first; t < p.tiles && ok; t += step, ++i) {
+        const int ab = i & 1, use = i >> 1;
+        if (use > 0 && !wait(&acc_empty[ab], (use - 1) & 1)) { if (leader) ch_fail(err, 2, 9, i); ok = false; break; }
         tc_fence_after_sync();
-        const bool last = (kb & 3) == 3 || kb == p.nkb - 1;
-        if (leader) {
-          const uint32_t base = smem_u32(ring + static_cast<size_t>(s) * stage_bytes);
-          const uint64_t da = umma_smem_desc_sw128(base), db = umma_smem_desc_sw128(base + kQmABytes);
-          const uint32_t id = idesc | (static_cast<uint32_t>(kb & 3) << 4) | (static_cast<uint32_t>(kb & 3) << 29);
-          const uint32_t sf = tmem + p.sf_col + (g & 1) * kQmSfCols;
+        const uint32_t d = tmem + ab * p.bn;
+        for (int st = 0; st < nst; ++st, ++it) {
+          const int s = it % S;
+          if (((st * KPS) & 3) == 0 && !wait(&sf_full[g & 1], (g >> 1) & 1)) { if (leader) ch_fail(err, 2, 10, g); ok = false; break; }
+          if (!wait(&full[s], (it / S) & 1)) { if (leader) ch_fail(err, 2, 11, it); ok = false; break; }
+          tc_fence_after_sync();
+          const int kb0 = st * KPS;
+          const bool last = ((kb0 + KPS) & 3) == 0 || st == nst - 1;     // of a group of four blocks
+          if (leader) {
+            const uint32_t base = smem_u32(ring + static_cast<size_t>(s) * stage_bytes);
+            const uint32_t sf = tmem + p.sf_col + (g & 1) * kQmSfCols;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) umma_mxf8(d, da + 2 * k, db + 2 * k, id, sf, sf + 4, kb > 0 || k > 0 ? 1u : 0u);
-          umma_commit(&empty[s]);
-          if (last) umma_commit(&sf_empty[g & 1]);
+            for (int j = 0; j < KPS; ++j) {
+              const int kb = kb0 + j;
+              if (kb >= p.nkb) break;
+              const uint64_t da = umma_smem_desc_sw128(base + j * block_bytes), db = umma_smem_desc_sw128(base + j * block_bytes + kQmABytes);
+              const uint32_t id = idesc | (static_cast<uint32_t>(kb & 3) << 4) | (static_cast<uint32_t>(kb & 3) << 29);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) umma_mxf8<PAIR>(d, da + 2 * k, db + 2 * k, id, sf, sf + 4, kb > 0 || k > 0 ? 1u : 0u);
+            }
+            if (PAIR) { umma_commit_pair(&empty[s]); if (last) umma_commit_pair(&sf_empty[g & 1]); }
+            else { umma_commit(&empty[s]); if (last) umma_commit(&sf_empty[g & 1]); }
+          }
+          if (last) ++g;
+          __syncwarp();
         }
-        if (last) ++g;
+        if (ok && leader) { if (PAIR) umma_commit_pair(&acc_full[ab]); else umma_commit(&acc_full[ab]); }
         __syncwarp();
       }
-      if (ok && leader) umma_commit(&acc_full[ab]);
-      __syncwarp();
     }
+    __syncwarp();
   } else if (warp < 6) {
     const int q = warp & 3, nb = p.bn / 32;
     int g = 0;
     for (int t = first; t < p.tiles && ok; t += step) {
-      const int n0 = t / p.tiles_m * 128, m0 = t % p.tiles_m * p.bn;
+      const int n0 = t / p.tiles_m * kRows + rank * 128, m0 = t % p.tiles_m * p.bn;
       for (int j = 0; j < groups; ++j, ++g) {
         uint32_t w[12];
 #pragma unroll
@@ -325,7 +393,7 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sf_full[g & 1]);
+        if (lane == 0) { if (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&sf_full[g & 1]), 0)); else mbar_arrive(&sf_full[g & 1]); }
       }
     }
   } else {
@@ -333,8 +401,8 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     int i = 0;
     OUT* out = static_cast<OUT*>(p.out);
     for (int t = first; t < p.tiles && ok; t += step, ++i) {
-      const int n = t / p.tiles_m * 128 + q * 32 + lane, m0 = t % p.tiles_m * p.bn;
-      const int ab = p.acc_bufs == 2 ? i & 1 : 0, use = p.acc_bufs == 2 ? i >> 1 : i;
+      const int n = t / p.tiles_m * kRows + rank * 128 + q * 32 + lane, m0 = t % p.tiles_m * p.bn;
+      const int ab = i & 1, use = i >> 1;
       if (!wait(&acc_full[ab], use & 1)) { if (lane == 0) ch_fail(err, 3, 9, i); ok = false; break; }
       tc_fence_after_sync();
       for (int c = 0; c < p.bn; c += 32) {
@@ -344,7 +412,7 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         if (c + 32 >= p.bn) {
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&acc_empty[ab]);
+          if (lane == 0) { if (PAIR) mbar_arrive_cluster_tmem(mapa_shared(smem_u32(&acc_empty[ab]), 0)); else mbar_arrive(&acc_empty[ab]); }
         }
         if (n < p.N) {
 #pragma unroll
@@ -356,8 +424,9 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
   }
   if (!ok) settle();   // copies that nobody waits for any more
   __syncthreads();
+  if (PAIR) { cluster_arrive(); cluster_wait(); }   // neither block leaves (or frees its columns) while the other's MMAs or arrivals may still reach it
   tc_fence_after_sync();
-  if (warp == 1) tmem_dealloc(tmem, p.tmem_cols);
+  if (warp == 1) { if (PAIR) tmem_dealloc_pair(tmem, p.tmem_cols); else tmem_dealloc(tmem, p.tmem_cols); }
 }
 
 }  // namespace csd
