@@ -1604,7 +1604,7 @@ int launch_quant_mma_t(csd_ctx* ctx, const CUtensorMap& tw, const CUtensorMap& t
     attr_done[ctx->device] = true;
   }
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3(grid); lc.blockDim = dim3(kQmThreads); lc.dynamicSmemBytes = smem; lc.stream = ctx->stream;
+  lc.gridDim = dim3(grid); lc.blockDim = dim3(quant_mma_threads(PAIR)); lc.dynamicSmemBytes = smem; lc.stream = ctx->stream;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -2718,7 +2718,7 @@ int csd_quant_matmul(csd_ctx* ctx, int M, int N, int K, const csd_quant* a, cons
   p.stages = (room - kQmFixed) / stage;
   if (p.stages > 8) p.stages = 8;
   p.sf_col = 2 * p.bn;
-  const int cols = p.sf_col + 2 * kQmSfCols;
+  const int cols = p.sf_col + kQmSfRing * kQmSfCols;
   for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
   const int most = pair ? ctx->num_sms / 2 : ctx->num_sms * (two ? 2 : 1);
   const int grid = (p.tiles < most ? p.tiles : most) * (pair ? 2 : 1);

@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const __grid_constant_
 //   warp 1      issues the MMAs (of a pair, the leader's): four of K = 32 a block under one scale byte (byte kb % 4 of the scale words)
 //   warps 2..5  bring the scales into tensor memory, a word (four blocks) per row: row 32 j + i at lane i, column j, in all
 //               four lane quarters; the token rows' scales into both blocks'
-//   warps 6..9  epilogue: a lane is a vocabulary row, a register a token
+//   warps 6..   epilogue: a lane is a vocabulary row, a register a token.  (Two tokens' columns packed to words by an exchange between lanes, for
+//               half as many stores, took 119 us where this takes 90: 576 x 65536 x 2048, bf16)
 struct QuantMmaParams {
   int M, N, nkb, ls;          // token rows, vocabulary rows, blocks of 128 columns, scale bytes a row
   int bn, stages, sf_col, tmem_cols, tiles_m, tiles;
@@ -218,9 +219,11 @@ struct QuantMmaParams {
   void* out;
   int64_t ldo;
 };
-constexpr int kQmThreads = 320;
+// threads: six warps and the epilogue's, of a pair's block eight (with four the MMAs waited for it where the sums are short: 2048 columns)
+constexpr int quant_mma_threads(bool pair) { return 32 * (6 + (pair ? 8 : 4)); }
 constexpr int kQmABytes = 128 * kQuantBlock;
 constexpr int kQmSfCols = 12;   // 4 of the weights' scales, up to 8 of the tokens'
+constexpr int kQmSfRing = 4;    // groups of scales in tensor memory (with two, the MMAs waited a seventh of their time for the next)
 constexpr int kQmFixed = 1024 + 256;
 
 // (+)= with e8m0 scales from tensor memory; the scale byte is chosen by the instruction descriptor
@@ -250,17 +253,18 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
 }
 
 template <typename OUT, bool PAIR, int KPS>
-__global__ void __launch_bounds__(kQmThreads, PAIR ? 1 : 2)
+__global__ void __launch_bounds__(quant_mma_threads(PAIR), PAIR ? 1 : 2)
 quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ QuantMmaParams p, int* err) {
+  constexpr int kEpi = PAIR ? 8 : 4;
   extern __shared__ uint8_t qm_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(qm_raw) + 1023) & ~uintptr_t(1023));
   const int b_rows = PAIR ? p.bn / 2 : p.bn;                      // token rows that this block loads
   const int block_bytes = kQmABytes + b_rows * kQuantBlock, stage_bytes = KPS * block_bytes, S = p.stages;
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + static_cast<size_t>(S) * stage_bytes);   // [8]
   uint64_t* empty = full + 8;       // [8]
-  uint64_t* sf_full = empty + 8;    // [2]
-  uint64_t* sf_empty = sf_full + 2; // [2]
-  uint64_t* acc_full = sf_empty + 2;   // [2]
+  uint64_t* sf_full = empty + 8;    // [kQmSfRing]
+  uint64_t* sf_empty = sf_full + kQmSfRing;
+  uint64_t* acc_full = sf_empty + kQmSfRing;   // [2]
   uint64_t* acc_empty = acc_full + 2;  // [2]
   uint32_t* tmem_s = reinterpret_cast<uint32_t*>(acc_empty + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -271,7 +275,8 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     tma_prefetch_desc(&tm_w);
     tma_prefetch_desc(&tm_a);
     for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sf_full[i], PAIR ? 8 : 4); mbar_init(&sf_empty[i], 1); mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], PAIR ? 8 : 4); }
+    for (int i = 0; i < kQmSfRing; ++i) { mbar_init(&sf_full[i], PAIR ? 8 : 4); mbar_init(&sf_empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], PAIR ? 2 * kEpi : kEpi); }
     fence_mbar_init();
   }
   __syncthreads();
@@ -342,14 +347,14 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
         const uint32_t d = tmem + ab * p.bn;
         for (int st = 0; st < nst; ++st, ++it) {
           const int s = it % S;
-          if (((st * KPS) & 3) == 0 && !wait(&sf_full[g & 1], (g >> 1) & 1)) { if (leader) ch_fail(err, 2, 10, g); ok = false; break; }
+          if (((st * KPS) & 3) == 0 && !wait(&sf_full[g % kQmSfRing], (g / kQmSfRing) & 1)) { if (leader) ch_fail(err, 2, 10, g); ok = false; break; }
           if (!wait(&full[s], (it / S) & 1)) { if (leader) ch_fail(err, 2, 11, it); ok = false; break; }
           tc_fence_after_sync();
           const int kb0 = st * KPS;
           const bool last = ((kb0 + KPS) & 3) == 0 || st == nst - 1;     // of a group of four blocks
           if (leader) {
             const uint32_t base = smem_u32(ring + static_cast<size_t>(s) * stage_bytes);
-            const uint32_t sf = tmem + p.sf_col + (g & 1) * kQmSfCols;
+            const uint32_t sf = tmem + p.sf_col + (g % kQmSfRing) * kQmSfCols;
 #pragma unroll
             for (int j = 0; j < KPS; ++j) {
               const int kb = kb0 + j;
@@ -359,8 +364,8 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
 #pragma unroll
               for (int k = 0; k < 4; ++k) umma_mxf8<PAIR>(d, da + 2 * k, db + 2 * k, id, sf, sf + 4, kb > 0 || k > 0 ? 1u : 0u);
             }
-            if (PAIR) { umma_commit_pair(&empty[s]); if (last) umma_commit_pair(&sf_empty[g & 1]); }
-            else { umma_commit(&empty[s]); if (last) umma_commit(&sf_empty[g & 1]); }
+            if (PAIR) { umma_commit_pair(&empty[s]); if (last) umma_commit_pair(&sf_empty[g % kQmSfRing]); }
+            else { umma_commit(&empty[s]); if (last) umma_commit(&sf_empty[g % kQmSfRing]); }
           }
           if (last) ++g;
           __syncwarp();
@@ -372,28 +377,47 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     __syncwarp();
   } else if (warp < 6) {
     const int q = warp & 3, nb = p.bn / 32;
+    // Words of four groups at a time: a row's lie together, and shared memory leaves the L1 cache too little to keep their lines
+    // from one group to the next (word by word, these loads took as much from L2 as a third of the operands).
+    const bool wide = (p.ls & 15) == 0 && ((reinterpret_cast<uintptr_t>(p.scale_w) | reinterpret_cast<uintptr_t>(p.scale_a)) & 15) == 0;
     int g = 0;
     for (int t = first; t < p.tiles && ok; t += step) {
       const int n0 = t / p.tiles_m * kRows + rank * 128, m0 = t % p.tiles_m * p.bn;
-      for (int j = 0; j < groups; ++j, ++g) {
-        uint32_t w[12];
+      for (int j4 = 0; j4 < groups && ok; j4 += 4) {
+        uint4 w[12];
 #pragma unroll
         for (int i = 0; i < 12; ++i) {
-          w[i] = 0x7f7f7f7fu;
+          w[i] = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
           const int row = i < 4 ? n0 + 32 * i + lane : m0 + 32 * (i - 4) + lane;
-          if (i < 4 ? row < p.N : i - 4 < nb && row < p.M)
-            w[i] = __ldg(reinterpret_cast<const uint32_t*>((i < 4 ? p.scale_w : p.scale_a) + static_cast<int64_t>(row) * p.ls) + j);
+          if (i < 4 ? row < p.N : i - 4 < nb && row < p.M) {
+            const uint32_t* src = reinterpret_cast<const uint32_t*>((i < 4 ? p.scale_w : p.scale_a) + static_cast<int64_t>(row) * p.ls) + j4;
+            if (wide) w[i] = __ldg(reinterpret_cast<const uint4*>(src));
+            else {
+              w[i].x = __ldg(src);
+              if (j4 + 1 < groups) w[i].y = __ldg(src + 1);
+              if (j4 + 2 < groups) w[i].z = __ldg(src + 2);
+              if (j4 + 3 < groups) w[i].w = __ldg(src + 3);
+            }
+          }
         }
-        if (g >= 2 && !wait(&sf_empty[g & 1], ((g >> 1) & 1) ^ 1)) { if (lane == 0) ch_fail(err, 2, 12, g); ok = false; break; }
-        tc_fence_after_sync();
-        const uint32_t at = tmem + p.sf_col + (g & 1) * kQmSfCols + (static_cast<uint32_t>(q * 32) << 16);
-        tmem_st4(at, w);
-        tmem_st4(at + 4, w + 4);
-        if (nb > 4) tmem_st4(at + 8, w + 8);
-        tmem_st_wait();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) { if (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&sf_full[g & 1]), 0)); else mbar_arrive(&sf_full[g & 1]); }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (j4 + k >= groups) break;
+          if (g >= kQmSfRing && !wait(&sf_empty[g % kQmSfRing], ((g / kQmSfRing) & 1) ^ 1)) { if (lane == 0) ch_fail(err, 2, 12, g); ok = false; break; }
+          tc_fence_after_sync();
+          uint32_t x[12];
+#pragma unroll
+          for (int i = 0; i < 12; ++i) x[i] = k == 0 ? w[i].x : k == 1 ? w[i].y : k == 2 ? w[i].z : w[i].w;
+          const uint32_t at = tmem + p.sf_col + (g % kQmSfRing) * kQmSfCols + (static_cast<uint32_t>(q * 32) << 16);
+          tmem_st4(at, x);
+          tmem_st4(at + 4, x + 4);
+          if (nb > 4) tmem_st4(at + 8, x + 8);
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) { if (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&sf_full[g % kQmSfRing]), 0)); else mbar_arrive(&sf_full[g % kQmSfRing]); }
+          ++g;
+        }
       }
     }
   } else {
@@ -405,19 +429,28 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
       const int ab = i & 1, use = i >> 1;
       if (!wait(&acc_full[ab], use & 1)) { if (lane == 0) ch_fail(err, 3, 9, i); ok = false; break; }
       tc_fence_after_sync();
-      for (int c = 0; c < p.bn; c += 32) {
+      auto drained = [&]() {                     // this warp has read all it needs: the MMAs may have the accumulator
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) { if (PAIR) mbar_arrive_cluster_tmem(mapa_shared(smem_u32(&acc_empty[ab]), 0)); else mbar_arrive(&acc_empty[ab]); }
+      };
+      const int c0 = (warp - 6) / 4 * 32;
+      if (c0 >= p.bn) drained();
+      for (int c = c0; c < p.bn; c += 32 * (kEpi / 4)) {
         float v[32];
         tmem_ld32(tmem + ab * p.bn + c + (static_cast<uint32_t>(q * 32) << 16), v);
         tmem_ld_wait();
-        if (c + 32 >= p.bn) {
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) { if (PAIR) mbar_arrive_cluster_tmem(mapa_shared(smem_u32(&acc_empty[ab]), 0)); else mbar_arrive(&acc_empty[ab]); }
-        }
+        if (c + 32 * (kEpi / 4) >= p.bn) drained();
         if (n < p.N) {
+          OUT* o = out + static_cast<int64_t>(m0 + c) * p.ldo + n;
+          const int rows = p.M - m0 - c;
+          if (rows >= 32) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (m0 + c + j < p.M) out[static_cast<int64_t>(m0 + c + j) * p.ldo + n] = quant_from_float<OUT>(v[j]);
+            for (int j = 0; j < 32; ++j, o += p.ldo) *o = quant_from_float<OUT>(v[j]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, o += p.ldo) if (j < rows) *o = quant_from_float<OUT>(v[j]);
+          }
         }
       }
     }
