@@ -1604,7 +1604,7 @@ int launch_quant_mma_t(csd_ctx* ctx, const CUtensorMap& tw, const CUtensorMap& t
     attr_done[ctx->device] = true;
   }
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3(grid); lc.blockDim = dim3(quant_mma_threads(PAIR)); lc.dynamicSmemBytes = smem; lc.stream = ctx->stream;
+  lc.gridDim = dim3(grid); lc.blockDim = dim3(kQmThreads); lc.dynamicSmemBytes = smem; lc.stream = ctx->stream;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -1618,7 +1618,7 @@ int launch_quant_mma_t(csd_ctx* ctx, const CUtensorMap& tw, const CUtensorMap& t
 
 template <typename OUT>
 int launch_quant_mma(csd_ctx* ctx, bool pair, const CUtensorMap& tw, const CUtensorMap& ta, const QuantMmaParams& p, int grid, size_t smem) {
-  return pair ? launch_quant_mma_t<OUT, true, 2>(ctx, tw, ta, p, grid, smem) : launch_quant_mma_t<OUT, false, 1>(ctx, tw, ta, p, grid, smem);
+  return pair ? launch_quant_mma_t<OUT, true, 2>(ctx, tw, ta, p, grid, smem) : launch_quant_mma_t<OUT, false, 4>(ctx, tw, ta, p, grid, smem);
 }
 
 }  // namespace
@@ -2705,22 +2705,21 @@ int csd_quant_matmul(csd_ctx* ctx, int M, int N, int K, const csd_quant* a, cons
   const int mt = (M + 223) / 224;
   p.bn = ((M + mt - 1) / mt + 31) / 32 * 32;
   p.tiles_m = (M + p.bn - 1) / p.bn;
-  // Pairs of blocks where the MMAs and not the weights' way from memory decide (QUANTRULE).
-  const bool pair = p.bn >= 96 && N >= 256;
+  // Pairs of blocks from 65 token rows on, single blocks with long stages below.  Pairs against single blocks, us: 448 x 50003 x 4096 90 and
+  // 112, 320 x 16384 x 4096 32 and 42, 96 x 50003 x 4096 52 and 56, 96 x 65536 x 2048 40 and 41, 128 x 32768 x 1024 15.2 and 15.2; stages of
+  // four blocks against pairs: 64 x 50003 x 4096 41 and 51, 64 x 16384 x 4096 14 and 19, 32 x 65536 x 2048 29 and 38, 32 x 8192 x 2048 9 and 13.
+  const bool pair = p.bn > 64;
   const int rows = pair ? 256 : 128;
   const int64_t tiles = static_cast<int64_t>((N + rows - 1) / rows) * p.tiles_m;
   if (tiles > INT32_MAX) return fail(ctx, CSD_ERR_UNSUPPORTED, "too many output tiles");
   p.tiles = static_cast<int>(tiles);
-  // few token rows leave room for two blocks an SM, whose loads and epilogues overlap
-  const int stage = pair ? 2 * (kQmABytes + p.bn / 2 * kQuantBlock) : kQmABytes + p.bn * kQuantBlock;
-  const bool two = !pair && p.bn <= 64;
-  const int room = two ? 113 * 1024 : 227 * 1024;
-  p.stages = (room - kQmFixed) / stage;
+  const int stage = pair ? 2 * (kQmABytes + p.bn / 2 * kQuantBlock) : 4 * (kQmABytes + p.bn * kQuantBlock);
+  p.stages = (227 * 1024 - kQmFixed) / stage;
   if (p.stages > 8) p.stages = 8;
   p.sf_col = 2 * p.bn;
   const int cols = p.sf_col + kQmSfRing * kQmSfCols;
   for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
-  const int most = pair ? ctx->num_sms / 2 : ctx->num_sms * (two ? 2 : 1);
+  const int most = pair ? ctx->num_sms / 2 : ctx->num_sms;
   const int grid = (p.tiles < most ? p.tiles : most) * (pair ? 2 : 1);
   const size_t smem = kQmFixed + static_cast<size_t>(p.stages) * stage;
   CUtensorMap tw, ta;

@@ -205,8 +205,8 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const __grid_constant_
 // fit the 512 tensor-memory columns): a single token row costs what reading the weights costs.
 // PAIR: two blocks of a cluster share each MMA (256 vocabulary rows, every block loads its own 128 and half of the token rows): a block of its own needs
 // 107 B a cycle of operands at 192 token rows, more than an SM takes from L2; in a pair it needs 75.
-//   warp 0      requests both operands by TMA, KPS blocks of 128 columns a stage (waiting for a stage and handing it back costs the issuing
-//               warp 300 to 500 cycles, about what one block's MMAs take)
+//   warp 0      requests both operands by TMA, KPS blocks of 128 columns a stage: waiting for a stage and handing it back costs the issuing
+//               warp 300 to 500 cycles, about what one block's MMAs take at 192 token rows and several times what they take at 32
 //   warp 1      issues the MMAs (of a pair, the leader's): four of K = 32 a block under one scale byte (byte kb % 4 of the scale words)
 //   warps 2..5  bring the scales into tensor memory, a word (four blocks) per row: row 32 j + i at lane i, column j, in all
 //               four lane quarters; the token rows' scales into both blocks'
@@ -219,8 +219,8 @@ struct QuantMmaParams {
   void* out;
   int64_t ldo;
 };
-// threads: six warps and the epilogue's, of a pair's block eight (with four the MMAs waited for it where the sums are short: 2048 columns)
-constexpr int quant_mma_threads(bool pair) { return 32 * (6 + (pair ? 8 : 4)); }
+constexpr int kQmEpi = 8;       // epilogue warps (with four the MMAs waited for them where the sums are short: 576 x 65536 x 2048 101 us, 93)
+constexpr int kQmThreads = 32 * (6 + kQmEpi);
 constexpr int kQmABytes = 128 * kQuantBlock;
 constexpr int kQmSfCols = 12;   // 4 of the weights' scales, up to 8 of the tokens'
 constexpr int kQmSfRing = 4;    // groups of scales in tensor memory (with two, the MMAs waited a seventh of their time for the next)
@@ -253,9 +253,8 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
 }
 
 template <typename OUT, bool PAIR, int KPS>
-__global__ void __launch_bounds__(quant_mma_threads(PAIR), PAIR ? 1 : 2)
+__global__ void __launch_bounds__(kQmThreads, 1)
 quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ QuantMmaParams p, int* err) {
-  constexpr int kEpi = PAIR ? 8 : 4;
   extern __shared__ uint8_t qm_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(qm_raw) + 1023) & ~uintptr_t(1023));
   const int b_rows = PAIR ? p.bn / 2 : p.bn;                      // token rows that this block loads
@@ -276,7 +275,7 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
     tma_prefetch_desc(&tm_a);
     for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int i = 0; i < kQmSfRing; ++i) { mbar_init(&sf_full[i], PAIR ? 8 : 4); mbar_init(&sf_empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], PAIR ? 2 * kEpi : kEpi); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], PAIR ? 2 * kQmEpi : kQmEpi); }
     fence_mbar_init();
   }
   __syncthreads();
@@ -436,11 +435,11 @@ quant_mma_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant
       };
       const int c0 = (warp - 6) / 4 * 32;
       if (c0 >= p.bn) drained();
-      for (int c = c0; c < p.bn; c += 32 * (kEpi / 4)) {
+      for (int c = c0; c < p.bn; c += 32 * (kQmEpi / 4)) {
         float v[32];
         tmem_ld32(tmem + ab * p.bn + c + (static_cast<uint32_t>(q * 32) << 16), v);
         tmem_ld_wait();
-        if (c + 32 * (kEpi / 4) >= p.bn) drained();
+        if (c + 32 * (kQmEpi / 4) >= p.bn) drained();
         if (n < p.N) {
           OUT* o = out + static_cast<int64_t>(m0 + c) * p.ldo + n;
           const int rows = p.M - m0 - c;
