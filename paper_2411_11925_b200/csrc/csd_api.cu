@@ -1557,11 +1557,13 @@ int check_quant(csd_ctx* ctx, const uint8_t* data, const uint8_t* scale, const c
 
 template <typename T, bool NORM>
 int launch_quant_rows(csd_ctx* ctx, int rows, const QuantRowsParams& p) {
-  // pieces of eight columns a thread: one up to 4096 columns, then two and (16-bit types: their registers) four; wider rows are read twice
-  const int pieces = p.ld / 8, nch = pieces <= 512 ? 1 : pieces <= 2048 ? 2 : pieces <= 4096 && sizeof(T) == 2 ? 4 : 0;
+  // pieces of eight columns a thread: one up to 4096 columns, two up to 8192, four (16-bit types) up to 16384; wider rows are read twice
+  constexpr int kWide = sizeof(T) == 2 ? 4 : 2;
+  const int pieces = p.ld / 8, nch = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : pieces <= 512 * kWide ? kWide : 0;
   const int threads = nch ? ((pieces + nch - 1) / nch + 31) / 32 * 32 : 1024;
-  auto kern = nch == 1 ? quant_rows_kernel<T, 1, NORM> : nch == 2 ? quant_rows_kernel<T, 2, NORM> : nch == 4 ? quant_rows_kernel<T, sizeof(T) == 2 ? 4 : 2, NORM> : quant_rows_kernel<T, 0, NORM>;
-  const int most = ctx->num_sms * (1024 / threads > 0 ? 1024 / threads : 1);   // resident at 64 registers
+  auto kern = nch == 1 ? quant_rows_kernel<T, 1, NORM> : nch == 2 ? quant_rows_kernel<T, 2, NORM> : nch == kWide ? quant_rows_kernel<T, kWide, NORM> : quant_rows_kernel<T, 0, NORM>;
+  const int fit = nch == 0 ? 1 : (nch <= 2 ? 1024 : 512) / threads;   // resident blocks an SM
+  const int most = ctx->num_sms * (fit > 0 ? fit : 1);
   rows = rows < most ? rows : most;
   return launch_short(ctx, ctx->stream, kern, rows, threads, 0, p);
 }

@@ -12,6 +12,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ptx.cuh"
 
 namespace csd {
@@ -32,39 +34,94 @@ struct QuantRowsParams {
   uint8_t *data, *scale;
 };
 
-__device__ __forceinline__ float quant_to_float(float v) { return v; }
-__device__ __forceinline__ float quant_to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float quant_to_float(__half v) { return __half2float(v); }
 template <typename T> __device__ __forceinline__ T quant_from_float(float v);
 template <> __device__ __forceinline__ float quant_from_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 quant_from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half quant_from_float<__half>(float v) { return __float2half_rn(v); }
 
-// Eight elements of a row from column `col` on as they lie, zeros behind the row's end; whole vectors where the row is 16-byte aligned.
+// Eight elements of a row from column `col` on as they lie, zeros behind the row's end.  16-bit rows that are not 16-byte aligned
+// are read as aligned vectors too, one more than the elements fill, and shifted (element by element a warp's loads touch every line eight
+// times: 154 us against 117 at 8192 x 5001 bf16 with residual; fp32, 216 and 236, goes by element); so do not pieces that would reach beyond the row.
 template <typename T> struct QuantRaw { __align__(16) T e[8]; };
 template <typename T>
-__device__ __forceinline__ void quant_load8(const T* row, int col, int K, bool aligned, QuantRaw<T>& v) {
-  if (aligned && col + 8 <= K) {
-    constexpr int kQ = sizeof(T) / 2;   // 16-byte vectors
+__device__ __forceinline__ void quant_load8(const T* row, int col, int K, QuantRaw<T>& v) {
+  constexpr int kQ = sizeof(T) / 2;   // 16-byte vectors
+  const uintptr_t a = reinterpret_cast<uintptr_t>(row + col);
+  const int off = static_cast<int>(a & 15);
+  uint32_t* out = reinterpret_cast<uint32_t*>(v.e);
+  if (off == 0 && col + 8 <= K) {
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(v.e)[i] = reinterpret_cast<const uint4*>(row + col)[i];
+    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(out)[i] = reinterpret_cast<const uint4*>(row + col)[i];
+  } else if (sizeof(T) == 2 && off != 0 && col > 0 && col + 8 + (16 - off) / static_cast<int>(sizeof(T)) <= K) {
+    const uint4* b = reinterpret_cast<const uint4*>(a - off);
+    __align__(16) uint32_t w[4 * kQ + 4];
+#pragma unroll
+    for (int i = 0; i <= kQ; ++i) reinterpret_cast<uint4*>(w)[i] = b[i];
+    const int sh = (off & 3) * 8;
+    auto shift = [&](auto first) {    // (the same for a whole row)
+      constexpr int k = decltype(first)::value;
+#pragma unroll
+      for (int i = 0; i < 4 * kQ; ++i) out[i] = sizeof(T) == 2 && k + i + 1 < 4 * kQ + 4 ? __funnelshift_r(w[k + i], w[k + i + 1], sh) : w[k + i];
+    };
+    switch (off >> 2) {
+      case 0: shift(std::integral_constant<int, 0>()); break;
+      case 1: shift(std::integral_constant<int, 1>()); break;
+      case 2: shift(std::integral_constant<int, 2>()); break;
+      default: shift(std::integral_constant<int, 3>());
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v.e[i] = col + i < K ? row[col + i] : quant_from_float<T>(0.0f);
   }
 }
+__device__ __forceinline__ void quant_floats(const QuantRaw<float>& v, float* h) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) h[i] = v.e[i];
+}
+__device__ __forceinline__ void quant_floats(const QuantRaw<__nv_bfloat16>& v, float* h) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(v.e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { h[2 * i] = __uint_as_float(w[i] << 16); h[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void quant_floats(const QuantRaw<__half>& v, float* h) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 f = __half22float2(reinterpret_cast<const __half2*>(v.e)[i]); h[2 * i] = f.x; h[2 * i + 1] = f.y; }
+}
+__device__ __forceinline__ void quant_round(const float* h, QuantRaw<float>& v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v.e[i] = h[i];
+}
+__device__ __forceinline__ void quant_round(const float* h, QuantRaw<__nv_bfloat16>& v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<__nv_bfloat162*>(v.e)[i] = __floats2bfloat162_rn(h[2 * i], h[2 * i + 1]);
+}
+__device__ __forceinline__ void quant_round(const float* h, QuantRaw<__half>& v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<__half2*>(v.e)[i] = __floats2half2_rn(h[2 * i], h[2 * i + 1]);
+}
 template <typename T>
-__device__ __forceinline__ void quant_store8(T* row, int col, int K, bool aligned, const float* v) {
-  if (aligned && col + 8 <= K) {
+__device__ __forceinline__ void quant_store8(T* row, int col, int K, const float* h) {
+  QuantRaw<T> v;
+  quant_round(h, v);
+  const uintptr_t a = reinterpret_cast<uintptr_t>(row + col);
+  if ((a & 15) == 0 && col + 8 <= K) {
     constexpr int kQ = sizeof(T) / 2;
-    __align__(16) T e[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = quant_from_float<T>(v[i]);
+    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(row + col)[i] = reinterpret_cast<uint4*>(v.e)[i];
+  } else if (sizeof(T) == 2 && col + 8 <= K) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(v.e);
+    if ((a & 3) == 0) {
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(row + col)[i] = reinterpret_cast<uint4*>(e)[i];
+      for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(row + col)[i] = w[i];
+    } else {
+      row[col] = v.e[0];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) reinterpret_cast<uint32_t*>(row + col + 1)[i] = __funnelshift_r(w[i], w[i + 1], 16);
+      row[col + 7] = v.e[7];
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) if (col + i < K) row[col + i] = quant_from_float<T>(v[i]);
+    for (int i = 0; i < 8; ++i) if (col + i < K) row[col + i] = v.e[i];
   }
 }
 
@@ -76,6 +133,8 @@ __device__ __forceinline__ uint32_t quant_scale_byte(uint32_t amax) {
   const int b = static_cast<int>((amax + 0x1fffffu) >> 23) - 8;
   return b > 0 ? static_cast<uint32_t>(b) : 0u;
 }
+// the larger one, a NaN if either is
+__device__ __forceinline__ float quant_max_nan(float a, float b) { float m; asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b)); return m; }
 __device__ __forceinline__ uint2 quant_pack8(const float* v, uint32_t byte) {
   if (byte == 255u) return make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
   const float inv = __uint_as_float((254u - byte) << 23);   // 2^(127 - byte), exact
@@ -90,53 +149,55 @@ __device__ __forceinline__ uint2 quant_pack8(const float* v, uint32_t byte) {
   return make_uint2(w[0], w[1]);
 }
 
+// Blocks of the most threads that an SM's registers hold.  Four pieces a thread take 112 registers; two of fp32 spill a little at 64, but
+// with 104 half as many blocks fit (8192 x 5000: 109 us and 152).
+template <typename T, int NCH> constexpr int quant_rows_resident() { return NCH == 1 || NCH == 2 ? 2 : 1; }
+
 // A block takes rows blockIdx.x, + gridDim.x, ...: the next row is requested before this one's reduction, so that its reads are under
 // way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, NORMFIG so; bound by
 // memory: 288 MB take 44 us at the rate of a copy).  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read
 // twice), 16 lanes a scale block.  Sums and the norm in fp32; the sum leaves rounded to the input's type, the norm uses it unrounded.
 template <typename T, int NCH, bool NORM>
-__global__ void __launch_bounds__(1024) quant_rows_kernel(const __grid_constant__ QuantRowsParams p) {
+__global__ void __launch_bounds__(NCH > 0 ? 512 : 1024, quant_rows_resident<T, NCH>()) quant_rows_kernel(const __grid_constant__ QuantRowsParams p) {
   __shared__ float part[2][32];
   constexpr int kN = NCH > 0 ? NCH : 1;
   const int tid = threadIdx.x, T_ = blockDim.x, pieces = p.ld / 8, lane = tid & 31;
   griddep_enter();
   const T* const wt = static_cast<const T*>(p.weight);
-  auto al = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
-  const bool aw = al(wt);
   auto row_x = [&](int64_t r) { return static_cast<const T*>(p.x) + r * p.ldx; };
   auto row_r = [&](int64_t r) { return static_cast<const T*>(p.residual) + r * p.ldr; };
   QuantRaw<T> vx[kN], vr[kN];
   auto fetch = [&](int64_t r, int j, int c) {
-    const T* x = row_x(r);
-    quant_load8(x, c * 8, p.K, al(x), vx[j]);
-    if (p.residual) { const T* y = row_r(r); quant_load8(y, c * 8, p.K, al(y), vr[j]); }
+    quant_load8(row_x(r), c * 8, p.K, vx[j]);
+    if (p.residual) quant_load8(row_r(r), c * 8, p.K, vr[j]);
   };
   auto take = [&](int j, float* h) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = quant_to_float(vx[j].e[i]);
+    quant_floats(vx[j], h);
     if (p.residual) {
+      float y[8];
+      quant_floats(vr[j], y);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] += quant_to_float(vr[j].e[i]);
+      for (int i = 0; i < 8; ++i) h[i] += y[i];
     }
   };
   auto put = [&](int64_t r, int c, float* h, float rstd) {   // (whole groups of 16 lanes are inside or outside)
-    if (p.sum) {
-      T* sum = static_cast<T*>(p.sum) + r * p.lds;
-      quant_store8(sum, c * 8, p.K, al(sum), h);
-    }
+    if (p.sum) quant_store8(static_cast<T*>(p.sum) + r * p.lds, c * 8, p.K, h);
     if (NORM) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] *= rstd;
       if (wt) {
         QuantRaw<T> w;
-        quant_load8(wt, c * 8, p.K, aw, w);
+        float y[8];
+        quant_load8(wt, c * 8, p.K, w);
+        quant_floats(w, y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] *= quant_to_float(w.e[i]);
+        for (int i = 0; i < 8; ++i) h[i] *= y[i];
       }
     }
-    uint32_t amax = 0;
+    float big = fabsf(h[0]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(h[i]) & 0x7fffffffu);
+    for (int i = 1; i < 8; ++i) big = quant_max_nan(big, fabsf(h[i]));
+    uint32_t amax = __float_as_uint(big) & 0x7fffffffu;
     const unsigned group = 0xffffu << (lane & 16);
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(group, amax, o));
