@@ -99,7 +99,10 @@ template <typename T> struct CatRow {
     head = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
     base = p - head;
   }
+  static constexpr bool kShared = false;
+  using Type = T;
   __device__ __forceinline__ int pieces() const { return (head + V + kCatPiece - 1) / kCatPiece; }
+  __device__ __forceinline__ T at(int i) const { return base[head + i]; }
   __device__ __forceinline__ bool whole(int v) const { const int first = v * kVec - head; return first >= 0 && first + kVec <= V; }
   __device__ __forceinline__ uint4 vec(int v) const { return __ldg(reinterpret_cast<const uint4*>(base) + v); }
   __device__ __forceinline__ bool some(int v) const { return v * kVec - head < V; }
@@ -127,17 +130,35 @@ __device__ __forceinline__ u64 cat_warp_max(u64 v) {
   return (static_cast<u64>(hi) << 32) | lo;
 }
 
+// A row that lies in shared memory, as the vectors of its aligned memory with what is outside masked.
+template <typename T> struct CatHeld {
+  static constexpr int kVec = CatType<T>::kVec;
+  static constexpr bool kShared = true;
+  using Type = T;
+  const uint4* data;
+  int head, V, vecs;
+  __device__ __forceinline__ bool whole(int v) const { return v < vecs; }
+  __device__ __forceinline__ bool some(int) const { return false; }
+  __device__ __forceinline__ uint4 vec(int v) const { return data[v]; }
+  __device__ __forceinline__ static uint4 none() { return CatRow<T>::none(); }
+  __device__ __forceinline__ uint4 edge(int) const { return none(); }
+  __device__ __forceinline__ int pieces() const { return (head + V + kCatPiece - 1) / kCatPiece; }
+  __device__ __forceinline__ T at(int i) const { return reinterpret_cast<const T*>(data)[head + i]; }
+};
+// What other blocks may have written, or this one in its own shared memory.
+template <bool SHARED, typename X> __device__ __forceinline__ X cat_get(const X* p) { return SHARED ? *p : __ldcg(p); }
+
 // f(logits, index of the first) for the vectors of pieces [p0, p1), a piece a warp; done(piece) after each.  Tokens outside the row are masked.
-template <typename T, typename F, typename D>
-__device__ __forceinline__ void cat_pieces(const CatRow<T>& row, int p0, int p1, F f, D done) {
-  constexpr int kVec = CatRow<T>::kVec, kIts = kCatPiece / (32 * kVec), kTwo = 4 / kIts;   // four vectors are requested at a time
+template <int NT, typename R, typename F, typename D>
+__device__ __forceinline__ void cat_pieces(const R& row, int p0, int p1, F f, D done) {
+  constexpr int kVec = R::kVec, kIts = kCatPiece / (32 * kVec), kTwo = 4 / kIts, kWarps = NT / 32;   // four vectors are requested at a time
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int p = p0 + warp; p < p1; p += kTwo * kCatWarps) {
+  for (int p = p0 + warp; p < p1; p += kTwo * kWarps) {
     uint4 raw[4];
     bool all = true;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int q = p + j / kIts * kCatWarps, v = (q * kIts + j % kIts) * 32 + lane;
+      const int q = p + j / kIts * kWarps, v = (q * kIts + j % kIts) * 32 + lane;
       const bool in = q < p1 && row.whole(v);
       all = all && in;
       if (in) raw[j] = row.vec(v);
@@ -145,28 +166,28 @@ __device__ __forceinline__ void cat_pieces(const CatRow<T>& row, int p0, int p1,
     if (!all) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int q = p + j / kIts * kCatWarps, v = (q * kIts + j % kIts) * 32 + lane;
+        const int q = p + j / kIts * kWarps, v = (q * kIts + j % kIts) * 32 + lane;
         if (q >= p1 || !row.whole(v)) raw[j] = q < p1 && row.some(v) ? row.edge(v) : row.none();
       }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int q = p + j / kIts * kCatWarps;
+      const int q = p + j / kIts * kWarps;
       if (q >= p1) break;
       float l[kVec];
-      CatType<T>::unpack(raw[j], l);
+      CatType<typename R::Type>::unpack(raw[j], l);
       f(l, ((q * kIts + j % kIts) * 32 + lane) * kVec - row.head);
       if (j % kIts == kIts - 1) done(q);
     }
   }
 }
-template <typename T, typename F>
-__device__ __forceinline__ void cat_each(const CatRow<T>& row, int p0, int p1, F f) { cat_pieces(row, p0, p1, f, [](int) {}); }
+template <int NT, typename R, typename F>
+__device__ __forceinline__ void cat_each(const R& row, int p0, int p1, F f) { cat_pieces<NT>(row, p0, p1, f, [](int) {}); }
 // The same where f gives a vector's weight: the pieces' sums go to seg; returns this thread's own sum.
-template <typename T, typename F>
-__device__ __forceinline__ u64 cat_sums(const CatRow<T>& row, int p0, int p1, u64* seg, F f) {
+template <int NT, typename R, typename F>
+__device__ __forceinline__ u64 cat_sums(const R& row, int p0, int p1, u64* seg, F f) {
   u64 all = 0, sum = 0;
-  cat_pieces(row, p0, p1, [&](const float* l, int idx) { sum += f(l, idx); }, [&](int q) {
+  cat_pieces<NT>(row, p0, p1, [&](const float* l, int idx) { sum += f(l, idx); }, [&](int q) {
     all += sum;
     sum = cat_warp_sum(sum);
     if ((threadIdx.x & 31) == 0) seg[q] = sum;
@@ -233,17 +254,24 @@ __device__ __forceinline__ u64 cat_bits(double v) { return static_cast<u64>(__do
 // Weight relative to the largest scaled logit: 2^44 exp(t - m), rounded; at most a few units above 2^44, 0 below 2^-45.
 __device__ __forceinline__ u64 cat_weight(float t, const CatScale& s, const double* tab) { return cat_bits(s.exp(t, tab)) - kCat256; }
 
-// Inclusive sum over the block's threads (exclusive = inclusive - v); part: kCatWarps values of shared memory.
-template <typename X> __device__ __forceinline__ X cat_block_scan(X v, X* part, X* total) {
+// Barriers of a block's first NT threads: what follows the passes over a row is dependent steps of few values, which more warps make slower.
+template <int NT> __device__ __forceinline__ void cat_sync() { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); }
+template <int NT> __device__ __forceinline__ bool cat_sync_or(bool x) {
+  uint32_t any;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(any) : "r"(static_cast<uint32_t>(x)), "n"(NT) : "memory");
+  return any != 0;
+}
+// Inclusive sum over the block's threads (exclusive = inclusive - v); part: a value a warp of shared memory.
+template <int NT, typename X> __device__ __forceinline__ X cat_block_scan(X v, X* part, X* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const X w = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += w; }
-  __syncthreads();
+  cat_sync<NT>();
   if (lane == 31) part[warp] = v;
-  __syncthreads();
+  cat_sync<NT>();
   X before = 0, all = 0;
 #pragma unroll
-  for (int i = 0; i < kCatWarps; ++i) { const X w = part[i]; if (i < warp) before += w; all += w; }
+  for (int i = 0; i < NT / 32; ++i) { const X w = part[i]; if (i < warp) before += w; all += w; }
   *total = all;
   return v + before;
 }
@@ -254,7 +282,7 @@ enum { CAT_DONE = 0, CAT_RANGE = 1, CAT_SEARCH = 2 };
 struct CatState {                                  // of a row
   uint32_t ticket[2], list_n;
   int mode;                                        // what is left to do for cat_range_kernel
-  float ta, tb, tk, te;                            // scaled logits: listed are [tb, ta) and [te, tk); weights wanted from ta up (and from tk up)
+  float da, db, dk, de;                            // distances from the largest: listed are [da, db) and [dk, de), weights wanted below da (and below dk)
   uint32_t at_a, n1, n_mid;
   int apart, upto, ends;
 };
@@ -283,15 +311,16 @@ struct CatParams {
 };
 
 // ---------------------------------------------------------------------------------------------------- shared memory
-struct CatShared {
+template <int NT> struct CatShared {
   __align__(16) uint32_t hist[2 * kCatBins];  // tokens per bin, sum of their places in it; later: sums of all pieces, words of a refinement
   __align__(16) u64 list[kCatList];           // candidates
-  u64 scan[kCatWarps];
-  uint2 scan2[kCatWarps];
-  u64 red[kCatWarps][3];
+  u64 scan[NT / 32];
+  uint2 scan2[NT / 32];
+  u64 red[32][3];
   double tab[16];
-  uint32_t rank[2 * kCatThreads];             // of the sort
+  uint32_t rank[2 * NT];                      // of the sort
   CatTop top;
+  CatState state;                             // of a row that one block holds
   // found by one thread, read by all
   u64 found_key, found_sum, found_upto, found_before[2];
   uint32_t found_n;
@@ -307,18 +336,19 @@ static_assert(2 * kCatBins * sizeof(uint32_t) >= kCatMaxPieces * sizeof(u64), "t
 static_assert(2 * kCatBins >= 4 * kCatSub, "a refinement's words do too");
 
 // Over the block's threads: the sums of a and b, the maximum of c.
-__device__ __forceinline__ void cat_reduce(CatShared& sh, u64& a, u64& b, u64& c) {
+template <int NT, int TAIL>
+__device__ __forceinline__ void cat_reduce(CatShared<TAIL>& sh, u64& a, u64& b, u64& c) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   a = cat_warp_sum(a); b = cat_warp_sum(b); c = cat_warp_max(c);
-  __syncthreads();
+  if (NT == TAIL) cat_sync<NT>(); else __syncthreads();
   if (lane == 0) { sh.red[warp][0] = a; sh.red[warp][1] = b; sh.red[warp][2] = c; }
-  __syncthreads();
-  a = 0; b = 0; c = 0;
-#pragma unroll
-  for (int i = 0; i < kCatWarps; ++i) { a += sh.red[i][0]; b += sh.red[i][1]; c = sh.red[i][2] > c ? sh.red[i][2] : c; }
+  if (NT == TAIL) cat_sync<NT>(); else __syncthreads();
+  const bool in = lane < NT / 32;
+  a = cat_warp_sum(in ? sh.red[lane][0] : 0); b = cat_warp_sum(in ? sh.red[lane][1] : 0); c = cat_warp_max(in ? sh.red[lane][2] : 0);
 }
 
 // Inclusive sums of a count and a weight over the block's threads.
+template <int NT>
 __device__ __forceinline__ void cat_block_scan2(uint32_t& n, float& w, uint2* part, float* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -328,11 +358,11 @@ __device__ __forceinline__ void cat_block_scan2(uint32_t& n, float& w, uint2* pa
     if (lane >= o) { n += x; w += y; }
   }
   if (lane == 31) part[warp] = make_uint2(n, __float_as_uint(w));
-  __syncthreads();
+  cat_sync<NT>();
   uint32_t bn = 0;
   float bw = 0.0f, all = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kCatWarps; ++i) {
+  for (int i = 0; i < NT / 32; ++i) {
     const uint2 x = part[i];
     if (i < warp) { bn += x.x; bw += __uint_as_float(x.y); }
     all += __uint_as_float(x.y);
@@ -341,127 +371,142 @@ __device__ __forceinline__ void cat_block_scan2(uint32_t& n, float& w, uint2* pa
   *total = all;
 }
 
-// Sorts list[0, n) ascending: by value into 256 buckets of equal width, then by counting within each (1.2 k cycles at 400 entries; each counting
+// Sorts list[0, n) ascending: by value into as many buckets of equal width as threads, then by counting within each (1.2 k cycles at 400 entries; each counting
 // all before it took 11 k, a bitonic network, whose every step is a round through shared memory, 20 k).  Where a bucket
 // holds too many (equals) the network does it, padded to a power of two; steps within 64 neighbours stay in one warp.
-__device__ __noinline__ void cat_sort(CatShared& sh, int n) {
+template <int NT>
+__device__ __noinline__ void cat_sort(CatShared<NT>& sh, int n) {
   u64* const list = sh.list;
   u64* const other = reinterpret_cast<u64*>(sh.hist);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  constexpr int kEach = kCatList / kCatThreads, kMost = 64;
-  static_assert(kCatThreads == 256, "a thread a bucket");
-  const int each = (n + kCatThreads - 1) / kCatThreads;
+  constexpr int kEach = kCatList / NT, kMost = 64;
+  if (n <= 96) {   // few: each counts all before it
+    const u64 key = tid < n ? list[tid] : 0;
+    int before = 0;
+    if (tid < n) {
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) before += list[j] < key;
+    }
+    cat_sync<NT>();
+    if (tid < n) list[before] = key;
+    cat_sync<NT>();
+    return;
+  }
+  const int each = (n + NT - 1) / NT;
   sh.rank[tid] = 0;
   uint32_t lo = 0xffffffffu, hi = 0;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     if (j >= each) break;
-    const int i = tid + j * kCatThreads;
+    const int i = tid + j * NT;
     if (i < n) { const uint32_t o = static_cast<uint32_t>(list[i] >> 32); lo = min(lo, o); hi = max(hi, o); }
   }
   lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi);
   if (lane == 0) sh.scan2[warp] = make_uint2(lo, hi);
-  __syncthreads();
+  cat_sync<NT>();
 #pragma unroll
-  for (int i = 0; i < kCatWarps; ++i) { const uint2 x = sh.scan2[i]; lo = min(lo, x.x); hi = max(hi, x.y); }
+  for (int i = 0; i < NT / 32; ++i) { const uint2 x = sh.scan2[i]; lo = min(lo, x.x); hi = max(hi, x.y); }
   const float first = cat_key_value(static_cast<u64>(lo) << 32), last = cat_key_value(static_cast<u64>(hi) << 32);
-  const float width = fmaxf(first - last, FLT_MIN), scale = fminf(__fdividef(255.0f, width), FLT_MAX);
+  const float width = fmaxf(first - last, FLT_MIN), scale = fminf(__fdividef(NT - 1.0f, width), FLT_MAX);
   uint32_t at[kEach];
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     if (j >= each) break;
-    const int i = tid + j * kCatThreads;
+    const int i = tid + j * NT;
     if (i < n) {
-      const uint32_t b = min(__float2uint_rd(fminf((first - cat_key_value(list[i])) * scale, 255.0f)), 255u);
+      const uint32_t b = min(__float2uint_rd(fminf((first - cat_key_value(list[i])) * scale, NT - 1.0f)), NT - 1u);
       at[j] = b << 16 | atomicAdd(&sh.rank[b], 1u);
     }
   }
-  __syncthreads();
+  cat_sync<NT>();
   const uint32_t own = sh.rank[tid];
-  if (!__syncthreads_or(own > kMost)) {
+  if (!cat_sync_or<NT>(own > kMost)) {
     uint32_t end = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const uint32_t x = __shfl_up_sync(0xffffffffu, end, o); if (lane >= o) end += x; }
     if (lane == 31) sh.scan2[warp].x = end;
-    __syncthreads();
+    cat_sync<NT>();
 #pragma unroll
-    for (int i = 0; i < kCatWarps; ++i) if (i < warp) end += sh.scan2[i].x;
-    sh.rank[kCatThreads + tid] = end;                // where a bucket ends
-    __syncthreads();
+    for (int i = 0; i < NT / 32; ++i) if (i < warp) end += sh.scan2[i].x;
+    sh.rank[NT + tid] = end;                // where a bucket ends
+    cat_sync<NT>();
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     if (j >= each) break;
-      const int i = tid + j * kCatThreads;
-      if (i < n) { const uint32_t b = at[j] >> 16; other[sh.rank[kCatThreads + b] - sh.rank[b] + (at[j] & 0xffffu)] = list[i]; }
+      const int i = tid + j * NT;
+      if (i < n) { const uint32_t b = at[j] >> 16; other[sh.rank[NT + b] - sh.rank[b] + (at[j] & 0xffffu)] = list[i]; }
     }
-    __syncthreads();
+    cat_sync<NT>();
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     if (j >= each) break;
-      const int i = tid + j * kCatThreads;
+      const int i = tid + j * NT;
       if (i < n) {
         const u64 key = list[i];
-        const uint32_t b = at[j] >> 16, to = sh.rank[kCatThreads + b], from = to - sh.rank[b];
+        const uint32_t b = at[j] >> 16, to = sh.rank[NT + b], from = to - sh.rank[b];
         uint32_t before = from;
         for (uint32_t k = from; k < to; ++k) before += other[k] < key;
         at[j] = before;
       }
     }
-    __syncthreads();
+    cat_sync<NT>();
     u64 key[kEach];
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) { if (j >= each) break; const int i = tid + j * kCatThreads; if (i < n) key[j] = list[i]; }
-    __syncthreads();
+    for (int j = 0; j < kEach; ++j) { if (j >= each) break; const int i = tid + j * NT; if (i < n) key[j] = list[i]; }
+    cat_sync<NT>();
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) { if (j >= each) break; const int i = tid + j * kCatThreads; if (i < n) list[at[j]] = key[j]; }
-    __syncthreads();
+    for (int j = 0; j < kEach; ++j) { if (j >= each) break; const int i = tid + j * NT; if (i < n) list[at[j]] = key[j]; }
+    cat_sync<NT>();
     return;
   }
   int P = 128;
   while (P < n) P <<= 1;
-  for (int i = n + tid; i < P; i += kCatThreads) list[i] = ~0ull;
-  __syncthreads();
+  for (int i = n + tid; i < P; i += NT) list[i] = ~0ull;
+  cat_sync<NT>();
   for (int size = 2; size <= P; size <<= 1)
     for (int stride = size >> 1; stride > 0; stride >>= 1) {
-      for (int i = tid; i < P / 2; i += kCatThreads) {
+      for (int i = tid; i < P / 2; i += NT) {
         const int a = ((i & ~(stride - 1)) << 1) | (i & (stride - 1)), b = a + stride;
         const u64 x = list[a], y = list[b];
         const bool up = (a & size) == 0;
         if ((x > y) == up) { list[a] = y; list[b] = x; }
       }
-      if (stride > 32 || (stride == 1 && size >= 64)) __syncthreads(); else __syncwarp();
+      if (stride > 32 || (stride == 1 && size >= 64)) cat_sync<NT>(); else __syncwarp();
     }
-  __syncthreads();
+  cat_sync<NT>();
 }
 
 // Whether this block is the last of its row's to come here; if so, what the others wrote before is visible to it.
-__device__ __forceinline__ bool cat_last(CatShared& sh, uint32_t* ticket, int splits) {
+template <int NT>
+__device__ __forceinline__ bool cat_last(CatShared<NT>& sh, uint32_t* ticket, int splits) {
   __threadfence();
-  __syncthreads();
+  cat_sync<NT>();
   if (threadIdx.x == 0) sh.last = splits == 1 || atomicAdd(ticket, 1u) == static_cast<uint32_t>(splits - 1);
-  __syncthreads();
+  cat_sync<NT>();
   if (!sh.last) return false;
   __threadfence();
   return true;
 }
 // This block's list goes to the row's in memory, ...
-__device__ __forceinline__ void cat_put_list(CatShared& sh, CatState* st, u64* list, int splits) {
-  __syncthreads();
+template <int NT>
+__device__ __forceinline__ void cat_put_list(CatShared<NT>& sh, CatState* st, u64* list, int splits) {
+  cat_sync<NT>();
   const uint32_t n = sh.list_n;
   if (splits == 1) return;
   if (threadIdx.x == 0 && n > 0) sh.base = atomicAdd(&st->list_n, n);
-  __syncthreads();
+  cat_sync<NT>();
   if (n > 0 && n <= kCatList)
-    for (uint32_t i = threadIdx.x; i < n; i += kCatThreads)
+    for (uint32_t i = threadIdx.x; i < n; i += NT)
       if (sh.base + i < kCatList) __stcg(list + sh.base + i, sh.list[i]);
 }
 // ... and comes back whole to the last block: the number of entries (more than kCatList: not all of them).
-__device__ __forceinline__ int cat_get_list(CatShared& sh, const CatState* st, const u64* list, int splits) {
-  __syncthreads();
+template <int NT>
+__device__ __forceinline__ int cat_get_list(CatShared<NT>& sh, const CatState* st, const u64* list, int splits) {
+  cat_sync<NT>();
   if (splits == 1) return static_cast<int>(min(sh.list_n, kCatList + 1u));
   const uint32_t n = min(__ldcg(&st->list_n), kCatList + 1u);
-  for (uint32_t i = threadIdx.x; i < min(n, static_cast<uint32_t>(kCatList)); i += kCatThreads) sh.list[i] = __ldcg(list + i);
-  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < min(n, static_cast<uint32_t>(kCatList)); i += NT) sh.list[i] = __ldcg(list + i);
+  cat_sync<NT>();
   return static_cast<int>(n);
 }
 
@@ -476,23 +521,23 @@ __device__ __forceinline__ u64 cat_target(float u, u64 total) {
 // The token at which the cumulative weight reaches target, by one block: seg has the sums of all pieces, without the weights of
 // the first `extra` entries of the list (listed(key)); the piece that holds the token is gone through again, a warp a vector.
 // weights(l, idx, w): of a vector's logits, as in the pass that formed the sums, listed tokens included.  One thread gets the token, the others -1.
-template <typename T, typename W, typename L>
-__device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, const u64* seg, u64 target, int extra, L listed, W weights) {
-  constexpr int kVec = CatRow<T>::kVec, kIts = kCatPiece / (32 * kVec), kEach = (kCatMaxPieces + kCatThreads - 1) / kCatThreads;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pieces = row.pieces(), each = (pieces + kCatThreads - 1) / kCatThreads;
+template <int NT, typename R, typename W, typename L>
+__device__ __forceinline__ int cat_locate(CatShared<NT>& sh, const R& row, const u64* seg, u64 target, int extra, L listed, W weights) {
+  constexpr int kVec = R::kVec, kIts = kCatPiece / (32 * kVec), kEach = (kCatMaxPieces + NT - 1) / NT;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pieces = row.pieces(), each = (pieces + NT - 1) / NT;
   // listed weights are added up in two words of 22 and 23 bits (a piece has 2^9 tokens)
   uint32_t *lo = sh.hist, *hi = sh.hist + kCatMaxPieces;
-  __syncthreads();
+  cat_sync<NT>();
   if (extra > 0) {
-    for (int i = tid; i < pieces; i += kCatThreads) { lo[i] = 0; hi[i] = 0; }
-    __syncthreads();
-    for (int i = tid; i < extra; i += kCatThreads) {
+    for (int i = tid; i < pieces; i += NT) { lo[i] = 0; hi[i] = 0; }
+    cat_sync<NT>();
+    for (int i = tid; i < extra; i += NT) {
       const u64 key = sh.list[i], w = listed(key);
       const int q = (static_cast<int>(static_cast<uint32_t>(key)) + row.head) / kCatPiece;
       atomicAdd(&lo[q], static_cast<uint32_t>(w) & 0x3fffffu);
       atomicAdd(&hi[q], static_cast<uint32_t>(w >> 22));
     }
-    __syncthreads();
+    cat_sync<NT>();
   }
   u64 x[kEach], s = 0, total;
 #pragma unroll
@@ -500,18 +545,18 @@ __device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, c
     const int i = tid * each + j;
     x[j] = 0;
     if (j < each && i < pieces) {
-      x[j] = __ldcg(seg + i);
+      x[j] = cat_get<R::kShared>(seg + i);
       if (extra > 0) x[j] += lo[i] + (static_cast<u64>(hi[i]) << 22);
     }
     s += x[j];
   }
-  u64 before = cat_block_scan<u64>(s, sh.scan, &total) - s;
+  u64 before = cat_block_scan<NT, u64>(s, sh.scan, &total) - s;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     if (before < target && before + x[j] >= target) { sh.found_piece = tid * each + j; sh.found_sum = before; }
     before += x[j];
   }
-  __syncthreads();
+  cat_sync<NT>();
   const int piece = sh.found_piece;
   u64 w[kVec], incl = 0;
   int idx = 0;
@@ -519,7 +564,7 @@ __device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, c
     const int v = (piece * kIts + warp) * 32 + lane;
     uint4 raw = row.whole(v) ? row.vec(v) : row.some(v) ? row.edge(v) : row.none();
     float l[kVec];
-    CatType<T>::unpack(raw, l);
+    CatType<typename R::Type>::unpack(raw, l);
     idx = v * kVec - row.head;
     weights(l, idx, w);
 #pragma unroll
@@ -529,7 +574,7 @@ __device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, c
     for (int o = 1; o < 32; o <<= 1) { const u64 y = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += y; }
     if (lane == 31) sh.scan[warp] = incl;
   }
-  __syncthreads();
+  cat_sync<NT>();
   int token = -1;
   if (warp < kIts) {
     before = sh.found_sum + incl - s;
@@ -547,9 +592,9 @@ __device__ __forceinline__ int cat_locate(CatShared& sh, const CatRow<T>& row, c
 // element in key order at which the running count reaches `count` (BY_WEIGHT: the running weight reaches `limit`) among keys
 // <= last, searched in ever narrower intervals [a, b] of keys.  Weights of a bin are summed in three words of 15 bits
 // each: 2^17 tokens fit, so a bin that holds more adds up its carries (the words are folded whenever 2^17 tokens have been read).
-template <bool BY_WEIGHT, typename T>
-__device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, float inv_t, const CatScale& sc, u64 last, u64 count, double limit) {
-  constexpr int kVec = CatRow<T>::kVec, kEach = kCatSub / kCatThreads, kFold = (1 << 17) / kCatPiece;
+template <bool BY_WEIGHT, int NT, typename R>
+__device__ __noinline__ u64 cat_refine(CatShared<NT>& sh, const R& row, float inv_t, const CatScale& sc, u64 last, u64 count, double limit) {
+  constexpr int kVec = R::kVec, kEach = kCatSub / NT, kFold = (1 << 17) / kCatPiece;
   const int tid = threadIdx.x, pieces = row.pieces();
   uint32_t* words = sh.hist + kCatSub;
   u64 a = 0, b = last;
@@ -558,10 +603,10 @@ __device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, floa
     const int shift = top > 10 ? top - 10 : 0;
     u64 n_before = 0, w_before = 0, none = 0, n[kEach] = {}, w[kEach] = {};
     for (int p0 = 0; p0 < pieces; p0 += kFold) {
-      __syncthreads();                               // nobody reads the arrays below any more
-      for (int i = tid; i < 4 * kCatSub; i += kCatThreads) sh.hist[i] = 0;
-      __syncthreads();
-      cat_each(row, p0, min(p0 + kFold, pieces), [&](const float* l, int idx) {
+      cat_sync<NT>();                               // nobody reads the arrays below any more
+      for (int i = tid; i < 4 * kCatSub; i += NT) sh.hist[i] = 0;
+      cat_sync<NT>();
+      cat_each<NT>(row, p0, min(p0 + kFold, pieces), [&](const float* l, int idx) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
           const float t = cat_scale(l[i], inv_t);
@@ -580,7 +625,7 @@ __device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, floa
           }
         }
       });
-      __syncthreads();
+      cat_sync<NT>();
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
         const int i = tid * kEach + j;
@@ -588,13 +633,13 @@ __device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, floa
         if (BY_WEIGHT) w[j] += words[i] + (static_cast<u64>(words[kCatSub + i]) << 15) + (static_cast<u64>(words[2 * kCatSub + i]) << 30);
       }
     }
-    cat_reduce(sh, n_before, w_before, none);
+    cat_reduce<NT>(sh, n_before, w_before, none);
     u64 own_n = 0, own_w = 0, all_n, all_w = 0;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) { own_n += n[j]; own_w += w[j]; }
-    u64 pn = cat_block_scan<u64>(own_n, sh.scan, &all_n) - own_n + n_before;
+    u64 pn = cat_block_scan<NT, u64>(own_n, sh.scan, &all_n) - own_n + n_before;
     u64 pw = w_before;
-    if (BY_WEIGHT) pw += cat_block_scan<u64>(own_w, sh.scan, &all_w) - own_w;
+    if (BY_WEIGHT) pw += cat_block_scan<NT, u64>(own_w, sh.scan, &all_w) - own_w;
     auto reached = [&](u64 cn, u64 cw) { return BY_WEIGHT ? static_cast<double>(cw) >= limit : cn >= count; };
     if (!reached(n_before + all_n, w_before + all_w)) return last;   // (all of them are kept)
 #pragma unroll
@@ -603,7 +648,7 @@ __device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, floa
       pn += n[j]; pw += w[j];
     }
     if (tid == 0) sh.list_n = 0;
-    __syncthreads();
+    cat_sync<NT>();
     a += static_cast<u64>(sh.found_a) << shift;
     const u64 span = (1ull << shift) - 1;
     b = b - a > span ? a + span : b;
@@ -611,7 +656,7 @@ __device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, floa
     pn = sh.found_before[0]; pw = sh.found_before[1];
     if (inside > kCatList) continue;
     // few enough to be sorted
-    cat_each(row, 0, pieces, [&](const float* l, int idx) {
+    cat_each<NT>(row, 0, pieces, [&](const float* l, int idx) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         const float t = cat_scale(l[i], inv_t);
@@ -619,20 +664,20 @@ __device__ __noinline__ u64 cat_refine(CatShared& sh, const CatRow<T>& row, floa
         if (t > -INFINITY && key >= a && key <= b) sh.append(key);
       }
     });
-    __syncthreads();
+    cat_sync<NT>();
     cat_sort(sh, inside);
     if (!BY_WEIGHT) return sh.list[count - pn - 1];
-    constexpr int kMine = kCatList / kCatThreads;
+    constexpr int kMine = kCatList / NT;
     u64 s = 0, total;
     for (int j = 0; j < kMine; ++j) { const int i = tid * kMine + j; if (i < inside) s += cat_weight(cat_key_value(sh.list[i]), sc, sh.tab); }
-    u64 before = cat_block_scan<u64>(s, sh.scan, &total) - s + pw;
+    u64 before = cat_block_scan<NT, u64>(s, sh.scan, &total) - s + pw;
     for (int j = 0; j < kMine; ++j) {
       const int i = tid * kMine + j;
       const u64 x = i < inside ? cat_weight(cat_key_value(sh.list[i]), sc, sh.tab) : 0;
       if (i < inside && !reached(0, before) && reached(0, before + x)) sh.found_key = sh.list[i];
       before += x;
     }
-    __syncthreads();
+    cat_sync<NT>();
     return sh.found_key;
   }
 }
@@ -652,15 +697,6 @@ __device__ __forceinline__ void cat_add_if(uint32_t* at, uint32_t v, uint32_t p,
 __device__ __forceinline__ uint32_t cat_place(float m, float l, float inv_t) {
   return __float2uint_rd(fminf((m - __fmul_rn(l, inv_t)) * (kCatPerUnit * (1 << kCatFrac)), 4095.0f * (1 << kCatFrac)));
 }
-// The least scaled logit that lies in a bin before b (in bin 0 none does).
-__device__ __forceinline__ float cat_threshold(float m, int b) {
-  if (b <= 0) return INFINITY;
-  const uint32_t at = static_cast<uint32_t>(b) << kCatFrac;
-  float t = m - static_cast<float>(b) / kCatPerUnit;
-  while (cat_place(m, t, 1.0f) < at && t > -FLT_MAX) t = nextafterf(t, -INFINITY);
-  while (cat_place(m, t, 1.0f) >= at && t < INFINITY) t = nextafterf(t, INFINITY);
-  return t;
-}
 struct CatRequest {   // what the caller asks of a row
   float inv_t, top_p;
   int want;           // top-k, 0: off
@@ -679,15 +715,11 @@ struct CatRequest {   // what the caller asks of a row
 // The least scaled logit that min-p keeps: the smallest fp32 number not below m + log(min_p).
 __device__ __forceinline__ float cat_least(const CatParams& p, int64_t r, float m) {
   const float mp = p.min_p ? p.min_p[r] : 0.0f;
-  if (!(mp > 0.0f)) return -INFINITY;
-  const double md = m, d = log(static_cast<double>(fminf(mp, 1.0f)));
-  float least = static_cast<float>(md + d);
-  while (static_cast<double>(least) - md < d) least = nextafterf(least, INFINITY);
-  while (static_cast<double>(nextafterf(least, -INFINITY)) - md >= d) least = nextafterf(least, -INFINITY);
-  return least;
+  return mp > 0.0f ? __double2float_ru(static_cast<double>(m) + log(static_cast<double>(fminf(mp, 1.0f)))) : -INFINITY;
 }
 // All parts' tops of a row, for every thread.
-__device__ __forceinline__ CatTop cat_tops(CatShared& sh, const CatWork& w, int row) {
+template <int NT>
+__device__ __forceinline__ CatTop cat_tops(CatShared<NT>& sh, const CatWork& w, int row) {
   if (threadIdx.x < 32) {
     uint32_t a = 0xffffffffu, b = 0, n = 0;
     for (int i = threadIdx.x; i < w.splits; i += 32) {
@@ -697,7 +729,7 @@ __device__ __forceinline__ CatTop cat_tops(CatShared& sh, const CatWork& w, int 
     a = __reduce_min_sync(0xffffffffu, a); b = __reduce_max_sync(0xffffffffu, b); n = __reduce_add_sync(0xffffffffu, n);
     if (threadIdx.x == 0) sh.top = CatTop{a, b, n, 0};
   }
-  __syncthreads();
+  cat_sync<NT>();
   return sh.top;
 }
 
@@ -719,12 +751,13 @@ struct CatKept {       // the conclusion
   int listed;          // so many of them are the first ones of the list, and not in the pieces' sums
 };
 // False: the list does not hold the cut.
-__device__ __noinline__ bool cat_resolve(CatShared& sh, const CatCut& x, const CatScale& sc, CatKept& out) {
+template <int NT>
+__device__ __noinline__ bool cat_resolve(CatShared<NT>& sh, const CatCut& x, const CatScale& sc, CatKept& out) {
   const int tid = threadIdx.x;
-  constexpr int kEach = kCatList / kCatThreads;
+  constexpr int kEach = kCatList / NT;
   cat_sort(sh, x.n);
   // a thread holds `each` entries in a row
-  const int each = x.n <= kCatThreads ? 1 : x.n <= 2 * kCatThreads ? 2 : kEach;
+  const int each = x.n <= NT ? 1 : x.n <= 2 * NT ? 2 : kEach;
   // where top-k ends in the list
   const int end_k = x.by_k ? static_cast<int>(x.k - x.n_above - x.n_mid) - 1 : x.n - 1;
   u64 s = 0, total;
@@ -735,9 +768,9 @@ __device__ __noinline__ bool cat_resolve(CatShared& sh, const CatCut& x, const C
     lw[i] = v;
     s += v;
   }
-  const u64 start = cat_block_scan<u64>(s, sh.scan, &total) - s;
+  const u64 start = cat_block_scan<NT, u64>(s, sh.scan, &total) - s;
   if (tid == 0) { sh.found_upto = 0; sh.found_sum = total; sh.found_listed = 0; }
-  __syncthreads();
+  cat_sync<NT>();
   u64 before = start;
   for (int j = 0; j < each; ++j) {
     const int i = tid * each + j;
@@ -745,7 +778,7 @@ __device__ __noinline__ bool cat_resolve(CatShared& sh, const CatCut& x, const C
     if (i == end_k) sh.found_sum = before;
     if (i == x.n1 - 1) sh.found_upto = before;
   }
-  __syncthreads();
+  cat_sync<NT>();
   double limit = INFINITY;
   if (x.by_p) limit = cat_limit(x.top_p, !x.by_k ? x.w_upto : x.apart ? x.w_upto + sh.found_sum - sh.found_upto : x.w_above + sh.found_sum);
   const int most = min(end_k, x.n1 - 1);
@@ -757,12 +790,12 @@ __device__ __noinline__ bool cat_resolve(CatShared& sh, const CatCut& x, const C
     before += lw[i];
   }
   mine = __reduce_add_sync(0xffffffffu, mine);
-  __syncthreads();                             // found_sum has been read
+  cat_sync<NT>();                             // found_sum has been read
   if ((tid & 31) == 0) sh.rank[tid >> 5] = mine;
-  __syncthreads();
+  cat_sync<NT>();
   int all = 0;
 #pragma unroll
-  for (int i = 0; i < kCatWarps; ++i) all += sh.rank[i];
+  for (int i = 0; i < NT / 32; ++i) all += sh.rank[i];
   const int last = all - 1;
   before = start + x.w_above;
   for (int j = 0; j < each; ++j) {
@@ -771,21 +804,21 @@ __device__ __noinline__ bool cat_resolve(CatShared& sh, const CatCut& x, const C
     // the cut is certain if the next one in the list is not kept, if top-k ends here, or if top-p's weight is reached here
     if (i == last && (last < most || last == end_k || x.ends || static_cast<double>(before) >= limit)) { sh.found_listed = all; sh.found_sum = before; }
   }
-  __syncthreads();
+  cat_sync<NT>();
   if (sh.found_listed == 0) return false;
   out.last = sh.list[last]; out.n = x.n_above + static_cast<u64>(all); out.w = sh.found_sum; out.listed = all;
-  __syncthreads();
+  cat_sync<NT>();
   return true;
 }
 
 // One pass over pieces: weights of the tokens that `bound` keeps, their sums by piece; for this thread their weight, number and last key.
-template <typename T>
-__device__ __forceinline__ u64 cat_keep(const CatRow<T>& row, int p0, int p1, u64* seg, float inv_t, const CatScale& sc, const double* tab, CatBound bound, u64& n, u64& last) {
-  constexpr int kVec = CatRow<T>::kVec;
+template <int NT, typename R>
+__device__ __forceinline__ u64 cat_keep(const R& row, int p0, int p1, u64* seg, float inv_t, const CatScale& sc, const double* tab, CatBound bound, u64& n, u64& last) {
+  constexpr int kVec = R::kVec;
   float end_t = INFINITY;   // the last token kept: the least, the highest index of its equals
   int end_i = 0;
   uint32_t count = 0;
-  const u64 w = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+  const u64 w = cat_sums<NT>(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
     u64 sum = 0;
 #pragma unroll
     for (int h = 0; h < kVec; h += 4) {     // four exponentials side by side
@@ -815,8 +848,8 @@ __device__ __forceinline__ u64 cat_keep(const CatRow<T>& row, int p0, int p1, u6
 }
 
 // Writes a row's summary and draws its token.  listed < kept.n: the pieces' sums are in seg.
-template <typename T>
-__device__ __forceinline__ void cat_finish(CatShared& sh, const CatParams& p, int64_t r, const CatRow<T>& row, const u64* seg, float inv_t, const CatScale& sc, float m, const CatKept& kept) {
+template <int NT, typename R>
+__device__ __forceinline__ void cat_finish(CatShared<NT>& sh, const CatParams& p, int64_t r, const R& row, const u64* seg, float inv_t, const CatScale& sc, float m, const CatKept& kept) {
   const int tid = threadIdx.x;
   const double norm = static_cast<double>(m) + log(static_cast<double>(kept.w)) - 44.0 * 0.69314718055994530942;
   const CatBound bound{cat_key_value(kept.last), static_cast<int>(static_cast<uint32_t>(kept.last))};
@@ -827,13 +860,13 @@ __device__ __forceinline__ void cat_finish(CatShared& sh, const CatParams& p, in
   if (!p.u) return;
   const u64 target = cat_target(p.u[r], kept.w);
   int found = -1;
-  if (kept.listed == static_cast<int>(kept.n) && kept.listed <= kCatThreads) {   // all of them are listed: each adds up those of smaller index
+  if (kept.listed == static_cast<int>(kept.n) && kept.listed <= NT) {   // all of them are listed: each adds up those of smaller index
     const int n = kept.listed;
     u64* w = reinterpret_cast<u64*>(sh.hist);
-    __syncthreads();
+    cat_sync<NT>();
     const u64 own = tid < n ? cat_weight(cat_key_value(sh.list[tid]), sc, sh.tab) : 0;
     w[tid] = own;
-    __syncthreads();
+    cat_sync<NT>();
     if (tid < n) {
       const uint32_t idx = static_cast<uint32_t>(sh.list[tid]);
       u64 before = 0;
@@ -844,7 +877,7 @@ __device__ __forceinline__ void cat_finish(CatShared& sh, const CatParams& p, in
     found = cat_locate(sh, row, seg, target, kept.listed, [&](u64 key) { return cat_weight(cat_key_value(key), sc, sh.tab); },
                        [&](const float* l, int idx, u64* w) {
 #pragma unroll
-      for (int i = 0; i < CatRow<T>::kVec; ++i) {
+      for (int i = 0; i < R::kVec; ++i) {
         const float t = cat_scale(l[i], inv_t);
         const u64 x = cat_weight(t, sc, sh.tab);
         w[i] = bound.kept(t, idx + i) ? x : 0;
@@ -853,27 +886,27 @@ __device__ __forceinline__ void cat_finish(CatShared& sh, const CatParams& p, in
   }
   if (found >= 0) {
     p.token[r] = found;
-    if (p.logp) p.logp[r] = static_cast<float>(static_cast<double>(cat_scale(cat_float(row.base[row.head + found]), inv_t)) - norm);
+    if (p.logp) p.logp[r] = static_cast<float>(static_cast<double>(cat_scale(cat_float(row.at(found)), inv_t)) - norm);
   }
 }
 
 // A row by one block, whatever it holds.
-template <typename T>
-__device__ __noinline__ void cat_search(CatShared& sh, const CatParams& p, int64_t r, const CatRow<T>& row, u64* seg, const CatRequest& q, bool by_k, const CatScale& sc, float m) {
-  constexpr int kVec = CatRow<T>::kVec;
+template <int NT, typename R>
+__device__ __noinline__ void cat_search(CatShared<NT>& sh, const CatParams& p, int64_t r, const R& row, u64* seg, const CatRequest& q, bool by_k, const CatScale& sc, float m) {
+  constexpr int kVec = R::kVec;
   const int pieces = row.pieces();
   u64 cut = ~0ull;
   if (by_k) cut = cat_refine<false>(sh, row, q.inv_t, sc, cut, q.want, 0.0);
   if (q.by_p) {
     u64 w = 0, none = 0, none2 = 0;
-    cat_each(row, 0, pieces, [&](const float* l, int idx) {
+    cat_each<NT>(row, 0, pieces, [&](const float* l, int idx) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         const float t = cat_scale(l[i], q.inv_t);
         if (cat_key(t, idx + i) <= cut) w += cat_weight(t, sc, sh.tab);
       }
     });
-    cat_reduce(sh, w, none, none2);
+    cat_reduce<NT>(sh, w, none, none2);
     cut = cat_refine<true>(sh, row, q.inv_t, sc, cut, 0, cat_limit(q.top_p, w));
   }
   const float least = cat_least(p, r, m);
@@ -881,8 +914,8 @@ __device__ __noinline__ void cat_search(CatShared& sh, const CatParams& p, int64
   if (cut != ~0ull) bound = CatBound{cat_key_value(cut), static_cast<int>(static_cast<uint32_t>(cut))};
   if (bound.value < least) bound = CatBound{least, INT_MAX};
   CatKept kept{};
-  u64 w = cat_keep(row, 0, pieces, seg, q.inv_t, sc, sh.tab, bound, kept.n, kept.last);
-  cat_reduce(sh, w, kept.n, kept.last);
+  u64 w = cat_keep<NT>(row, 0, pieces, seg, q.inv_t, sc, sh.tab, bound, kept.n, kept.last);
+  cat_reduce<NT>(sh, w, kept.n, kept.last);
   kept.w = w;
   __threadfence();
   cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
@@ -958,47 +991,51 @@ __global__ void __launch_bounds__(kCatThreads) cat_top_kernel(const __grid_const
 __device__ __forceinline__ float cat_exp2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // From a row's counts: between which bins top-p ends, and in which top-k; what cat_range_kernel has to look at.
-__device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatState* st, const CatRequest& q, uint32_t live, float m, float least) {
+template <bool SHARED, int NT>
+__device__ __noinline__ void cat_bins(CatShared<NT>& sh, const uint32_t* hist, CatState* st, const CatRequest& q, uint32_t live, float m, float least) {
   const int tid = threadIdx.x;
-  constexpr int kEach = kCatBins / kCatThreads;
+  constexpr int kEach = kCatBins / NT;
   const bool by_k = q.want > 0 && static_cast<uint32_t>(q.want) < live;
   const uint32_t k = q.want;
   uint32_t n[kEach], own_n = 0;
   float e[kEach], own_e = 0.0f;
+  uint32_t hn[kEach], fn[kEach];
 #pragma unroll
-  for (int j = 0; j < kEach; j += 4) {
-    const uint4 h = __ldcg(reinterpret_cast<const uint4*>(hist) + (tid * kEach + j) / 4);
-    const uint4 f = __ldcg(reinterpret_cast<const uint4*>(hist + kCatBins) + (tid * kEach + j) / 4);
-    const uint32_t hn[4] = {h.x, h.y, h.z, h.w}, fn[4] = {f.x, f.y, f.z, f.w};
+  for (int j = 0; j < kEach; j += 2) {
+    const uint2 h = cat_get<SHARED>(reinterpret_cast<const uint2*>(hist) + (tid * kEach + j) / 2);
+    const uint2 f = cat_get<SHARED>(reinterpret_cast<const uint2*>(hist + kCatBins) + (tid * kEach + j) / 2);
+    hn[j] = h.x; hn[j + 1] = h.y; fn[j] = f.x; fn[j + 1] = f.y;
+  }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      n[j + i] = hn[i];
-      const float c = static_cast<float>(hn[i]);
-      const float place = tid * kEach + j + i + (hn[i] ? __fdividef(static_cast<float>(fn[i]) + 0.5f * c, c * (1 << kCatFrac)) : 0.0f);
-      e[j + i] = q.by_p ? c * cat_exp2(-static_cast<float>(kLog2e) / kCatPerUnit * place) : 0.0f;
-      own_n += n[j + i]; own_e += e[j + i];
-    }
+  for (int j = 0; j < kEach; ++j) {
+    n[j] = hn[j];
+    const float c = static_cast<float>(hn[j]);
+    const float place = tid * kEach + j + (hn[j] ? __fdividef(static_cast<float>(fn[j]) + 0.5f * c, c * (1 << kCatFrac)) : 0.0f);
+    e[j] = q.by_p ? c * cat_exp2(-static_cast<float>(kLog2e) / kCatPerUnit * place) : 0.0f;
+    own_n += n[j]; own_e += e[j];
   }
   uint32_t cum0 = own_n;
   float mass0 = own_e, all_mass;
   if (tid == 0) { sh.found_a = sh.found_b = sh.found_k = kCatBins; sh.found_prev = -1; }
-  cat_block_scan2(cum0, mass0, sh.scan2, &all_mass);
+  cat_block_scan2<NT>(cum0, mass0, sh.scan2, &all_mass);
   cum0 -= own_n; mass0 -= own_e;
-  // the bin in which top-k ends, and bounds of the weight that top-p refers to
+  // the bin in which top-k ends, and bounds of the weight that top-p refers to (the thread that holds it looks for it)
   float lo = all_mass, hi = all_mass;
   if (by_k) {
-    uint32_t cum = cum0;
-    float mass = mass0;
+    if (cum0 < k && cum0 + own_n >= k) {
+      uint32_t cum = cum0;
+      float mass = mass0;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if (cum < k && cum + n[j] >= k) {
-        sh.found_k = tid * kEach + j;
-        const float w = e[j] / n[j] * (k - cum);   // a part of the bin: weights within exp(+-1/64)
-        sh.found_lo = mass + w * 0.984f; sh.found_hi = mass + w * 1.016f;
+      for (int j = 0; j < kEach; ++j) {
+        if (cum < k && cum + n[j] >= k) {
+          sh.found_k = tid * kEach + j;
+          const float w = e[j] / n[j] * (k - cum);   // a part of the bin: weights within exp(+-1/64)
+          sh.found_lo = mass + w * 0.984f; sh.found_hi = mass + w * 1.016f;
+        }
+        cum += n[j]; mass += e[j];
       }
-      cum += n[j]; mass += e[j];
     }
-    __syncthreads();
+    cat_sync<NT>();
     lo = sh.found_lo; hi = sh.found_hi;
   }
   const int bin_k = sh.found_k;
@@ -1010,17 +1047,20 @@ __device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatSt
     constexpr float kLo = 1.0f - 3.2e-4f, kHi = 1.0f + 3.5e-4f;
     constexpr float kNear = 1.0f + 1e-5f;   // (the sum up to a bin is not the same number at its end and at the next one's start)
     const float lim_lo = q.top_p * lo * kLo, lim_hi = q.top_p * hi * kHi;
-    float mass = mass0;
+    const float end0 = mass0 + own_e;
+    if (((mass0 * kHi < lim_lo * kNear || tid == 0) && end0 * kHi >= lim_lo) || ((mass0 * kLo < lim_hi * kNear || tid == 0) && end0 * kLo >= lim_hi)) {
+      float mass = mass0;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int b = tid * kEach + j;
-      const float end = j < kEach - 1 ? mass + e[j] : mass0 + own_e;
-      // top-p ends in the first bin at whose end its weight is reached: not before a, not behind b
-      if ((mass * kHi < lim_lo * kNear || b == 0) && end * kHi >= lim_lo) atomicMin(&sh.found_a, b);
-      if ((mass * kLo < lim_hi * kNear || b == 0) && end * kLo >= lim_hi) atomicMin(&sh.found_b, b);
-      mass = end;
+      for (int j = 0; j < kEach; ++j) {
+        const int b = tid * kEach + j;
+        const float end = j < kEach - 1 ? mass + e[j] : end0;
+        // top-p ends in the first bin at whose end its weight is reached: not before a, not behind b
+        if ((mass * kHi < lim_lo * kNear || b == 0) && end * kHi >= lim_lo) atomicMin(&sh.found_a, b);
+        if ((mass * kLo < lim_hi * kNear || b == 0) && end * kLo >= lim_hi) atomicMin(&sh.found_b, b);
+        mass = end;
+      }
     }
-    __syncthreads();
+    cat_sync<NT>();
     bin_a = sh.found_a; bin_b = sh.found_b;
     if (by_k && bin_b >= bin_k) { bin_b = bin_k; bin_a = min(bin_a, bin_k); }   // top-k's end lies among the bins of top-p's
   }
@@ -1034,22 +1074,24 @@ __device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatSt
       bin_a = min(bin_a, bin_m);
 #pragma unroll
       for (int j = 0; j < kEach; ++j) if (n[j] && tid * kEach + j < bin_a) atomicMax(&sh.found_prev, tid * kEach + j);
-      __syncthreads();
+      cat_sync<NT>();
       if (sh.found_prev >= 0) bin_a = sh.found_prev;
     }
   }
   const bool known = bin_b < kCatBins && bin_a <= bin_b && (!by_k || bin_k < kCatBins || (ends && !q.by_p));
-  uint32_t cum = cum0;
+  if (tid == bin_a / kEach || tid == bin_b / kEach || tid == bin_k / kEach) {
+    uint32_t cum = cum0;
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    const int b = tid * kEach + j;
-    if (b == bin_a) sh.at_a = cum;
-    if (b == bin_k) sh.at_k = cum;
-    cum += n[j];
-    if (b == bin_b) sh.at_b = cum;
-    if (b == bin_k) sh.end_k = cum;
+    for (int j = 0; j < kEach; ++j) {
+      const int b = tid * kEach + j;
+      if (b == bin_a) sh.at_a = cum;
+      if (b == bin_k) sh.at_k = cum;
+      cum += n[j];
+      if (b == bin_b) sh.at_b = cum;
+      if (b == bin_k) sh.end_k = cum;
+    }
   }
-  __syncthreads();
+  cat_sync<NT>();
   const bool apart = by_k && q.by_p && bin_k > bin_b;   // top-k ends in a bin of its own, and top-p refers to what is before
   if (tid == 0) {
     const bool fits = known && sh.at_b - sh.at_a + (apart ? sh.end_k - sh.at_k : 0) <= kCatList;
@@ -1057,14 +1099,121 @@ __device__ __noinline__ void cat_bins(CatShared& sh, const uint32_t* hist, CatSt
     st->at_a = sh.at_a; st->n1 = sh.at_b - sh.at_a; st->n_mid = apart ? sh.at_k - sh.at_b : 0;
     st->apart = apart; st->upto = q.by_p && (apart || !by_k); st->ends = ends;
   }
-  if (tid < 4 * 32 && (tid & 31) == 0) (&st->ta)[tid / 32] = cat_threshold(m, tid == 0 ? bin_a : tid == 32 ? bin_b + 1 : tid == 64 ? bin_k : bin_k + 1);
+  // (a token lies in a bin before b iff its distance is below b / 64: the places are products by a power of two)
+  if (tid == 0) { st->da = bin_a / kCatPerUnit; st->db = (bin_b + 1) / kCatPerUnit; st->dk = bin_k / kCatPerUnit; st->de = (bin_k + 1) / kCatPerUnit; }
+}
+
+// Counts tokens of pieces [p0, p1) by distance from the largest, and adds up their places: for bins tid * kEach + j.  One addition a token: count and
+// place in one word, taken apart before 2^13 tokens could overflow it.
+template <int NT, int TAIL, typename R>
+__device__ __forceinline__ void cat_count(CatShared<TAIL>& sh, const R& row, int p0, int p1, const CatRequest& q, float m, uint32_t* n, uint32_t* f) {
+  constexpr int kVec = R::kVec, kEach = kCatBins / NT, kMost = (1 << 13) / kCatPiece;
+  const int tid = threadIdx.x;
+  uint32_t* pack = reinterpret_cast<uint32_t*>(sh.list);
+  uint2* own = reinterpret_cast<uint2*>(pack) + tid * kEach / 2;
+#pragma unroll
+  for (int j = 0; j < kEach; j += 2) { own[j / 2] = make_uint2(0, 0); n[j] = n[j + 1] = f[j] = f[j + 1] = 0; }
+  for (int q0 = p0; q0 < p1; q0 += kMost) {
+    __syncthreads();
+    cat_each<NT>(row, q0, min(q0 + kMost, p1), [&](const float* l, int) {
+      uint32_t at[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) at[i] = cat_place(m, l[i], q.inv_t);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) cat_add_if(pack + (at[i] >> kCatFrac), (1u << kCatPack) | (at[i] & ((1u << kCatFrac) - 1)), at[i], kCatBins << kCatFrac);
+    });
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; j += 2) {
+      const uint2 x = own[j / 2];
+      own[j / 2] = make_uint2(0, 0);
+      n[j] += x.x >> kCatPack; f[j] += x.x & ((1u << kCatPack) - 1);
+      n[j + 1] += x.y >> kCatPack; f[j + 1] += x.y & ((1u << kCatPack) - 1);
+    }
+  }
+}
+
+// The weights that a row's state asks for: those above the bins in question by piece, and this thread's sums of these and (where top-p refers to
+// them) of all before top-k's bin; the tokens of the bins in question go to the list.
+template <int NT, int TAIL, typename R>
+__device__ __forceinline__ u64 cat_weights(CatShared<TAIL>& sh, const R& row, int p0, int p1, u64* seg, const CatRequest& q, const CatScale& sc, float m, const CatState& st, u64& w_upto) {
+  constexpr int kVec = R::kVec;
+  const float da = st.da, db = st.db, dk = st.dk, de = st.de;
+  const bool apart = st.apart != 0, upto = st.upto != 0;
+  if (upto && !apart && sc.base == 0.0f) {
+    // top-p without top-k, the common case: every token's weight is wanted
+    return cat_sums<NT>(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+      u64 above = 0;
+      bool list = false;
+#pragma unroll
+      for (int h = 0; h < kVec; h += 4) {   // four exponentials side by side
+        float t[4];
+        u64 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { t[i] = __fmul_rn(l[h + i], q.inv_t); x[i] = cat_bits(sc.exp0(t[i], sh.tab)); }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w_upto += x[i];
+          const float d = m - t[i];
+          if (d < da) above += x[i] - kCat256;
+          list = list || (d < db && !(d < da));
+        }
+        w_upto -= 4 * kCat256;
+      }
+      if (list) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const float d = m - __fmul_rn(l[i], q.inv_t);
+          if (d < db && !(d < da)) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+        }
+      }
+      return above;
+    });
+  } else {
+    const float need = upto ? dk : da;
+    return cat_sums<NT>(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+      u64 above = 0;
+      bool list = false;
+#pragma unroll
+      for (int h = 0; h < kVec; h += 4) {
+        float t[4];
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          t[i] = __fmul_rn(l[h + i], q.inv_t);
+          const float d = m - t[i];
+          any = any || d < need || (upto && !apart);
+          list = list || (d < db && !(d < da)) || (apart && d < de && !(d < dk));
+        }
+        if (!__any_sync(0xffffffffu, any)) continue;
+        u64 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = cat_bits(sc.exp(t[i], sh.tab)) - kCat256;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float d = m - t[i];
+          if (d < da) above += x[i];
+          if (upto && (!apart || d < dk)) w_upto += x[i];
+        }
+      }
+      if (list) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const float d = m - __fmul_rn(l[i], q.inv_t);
+          if ((d < db && !(d < da)) || (apart && d < de && !(d < dk))) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+        }
+      }
+      return above;
+    });
+  }
 }
 
 // Rows without top-k and top-p: everything that is left to do.  Rows with a small top-k: the tokens above the threshold, of which the
 // row's last block derives everything.  Other rows: counts by distance from the largest.
 template <typename T>
 __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_constant__ CatParams p) {
-  __shared__ CatShared sh;
+  __shared__ CatShared<kCatThreads> sh;
+  constexpr int NT = kCatThreads;
   const int tid = threadIdx.x, row_i = blockIdx.x / p.w.splits, split = blockIdx.x % p.w.splits;
   const int64_t r = p.r0 + row_i;
   constexpr int kVec = CatRow<T>::kVec;
@@ -1090,8 +1239,8 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
     const CatScale sc(m, kCatFloor);
     const float least = cat_least(p, r, m);
     CatKept kept{};
-    u64 w = cat_keep(row, p0, p1, seg, q.inv_t, sc, sh.tab, least > -INFINITY ? CatBound{least, INT_MAX} : CatBound{-INFINITY, INT_MIN}, kept.n, kept.last);
-    cat_reduce(sh, w, kept.n, kept.last);
+    u64 w = cat_keep<NT>(row, p0, p1, seg, q.inv_t, sc, sh.tab, least > -INFINITY ? CatBound{least, INT_MAX} : CatBound{-INFINITY, INT_MIN}, kept.n, kept.last);
+    cat_reduce<NT>(sh, w, kept.n, kept.last);
     u64* tot = p.w.tot + static_cast<int64_t>(row_i) * p.w.splits * 3;
     if (tid == 0) { __stcg(tot + split * 3, w); __stcg(tot + split * 3 + 1, kept.n); __stcg(tot + split * 3 + 2, kept.last); }
     if (!cat_last(sh, &st->ticket[0], p.w.splits)) return;
@@ -1101,12 +1250,12 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
       const u64 k = __ldcg(tot + i * 3 + 2);
       kept.last = k > kept.last ? k : kept.last;
     }
-    cat_reduce(sh, w, kept.n, kept.last);
+    cat_reduce<NT>(sh, w, kept.n, kept.last);
     kept.w = w;
     cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
   } else if (by_k && q.few && top.tau < 0xff800000u) {
     const float from = cat_key_value(static_cast<u64>(top.tau) << 32);
-    cat_each(row, p0, p1, [&](const float* l, int idx) {
+    cat_each<NT>(row, p0, p1, [&](const float* l, int idx) {
       float big = l[0];
 #pragma unroll
       for (int i = 1; i < kVec; ++i) big = fmaxf(big, l[i]);
@@ -1126,38 +1275,15 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
     if (x.n <= kCatList && cat_resolve(sh, x, sc, kept)) cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
     else cat_search(sh, p, r, row, seg, q, by_k, sc, m);   // (many tokens above the threshold: rows in order, many equals)
   } else {
-    // one addition a token: count and place in one word, taken apart before 2^13 tokens could overflow it
-    uint32_t* pack = reinterpret_cast<uint32_t*>(sh.list);
-    constexpr int kEach = kCatBins / kCatThreads, kMost = (1 << 13) / kCatPiece;
-    uint32_t n[kEach] = {}, f[kEach] = {};               // of bins tid * kEach + j
-#pragma unroll
-    for (int j = 0; j < kEach; j += 4) reinterpret_cast<uint4*>(pack)[(tid * kEach + j) / 4] = make_uint4(0, 0, 0, 0);
-    for (int q0 = p0; q0 < p1; q0 += kMost) {
-      __syncthreads();
-      cat_each(row, q0, min(q0 + kMost, p1), [&](const float* l, int) {
-        uint32_t at[kVec];
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) at[i] = cat_place(m, l[i], q.inv_t);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) cat_add_if(pack + (at[i] >> kCatFrac), (1u << kCatPack) | (at[i] & ((1u << kCatFrac) - 1)), at[i], kCatBins << kCatFrac);
-      });
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kEach; j += 4) {
-        uint4* at = reinterpret_cast<uint4*>(pack) + (tid * kEach + j) / 4;
-        const uint4 x = *at;
-        *at = make_uint4(0, 0, 0, 0);
-        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { n[j + i] += y[i] >> kCatPack; f[j + i] += y[i] & ((1u << kCatPack) - 1); }
-      }
-    }
+    constexpr int kEach = kCatBins / NT;
+    uint32_t n[kEach], f[kEach];               // of bins tid * kEach + j
+    cat_count<NT>(sh, row, p0, p1, q, m, n, f);
     uint32_t* hist = p.w.hist + static_cast<int64_t>(row_i) * 2 * kCatBins;
 #pragma unroll
     for (int j = 0; j < kEach; ++j)
       if (n[j]) { atomicAdd(hist + tid * kEach + j, n[j]); if (q.by_p) atomicAdd(hist + kCatBins + tid * kEach + j, f[j]); }
     if (!cat_last(sh, &st->ticket[0], p.w.splits)) return;
-    cat_bins(sh, hist, st, q, top.live, m, cat_least(p, r, m));
+    cat_bins<false>(sh, hist, st, q, top.live, m, cat_least(p, r, m));
   }
 }
 
@@ -1165,10 +1291,10 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
 // piece, and the tokens of those bins, of which the row's last block derives the cut.  Bound by the exponentials: 4 cycles a warp of tokens in fp64.
 template <typename T>
 __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_constant__ CatParams p) {
-  __shared__ CatShared sh;
+  __shared__ CatShared<kCatThreads> sh;
+  constexpr int NT = kCatThreads;
   const int tid = threadIdx.x, row_i = blockIdx.x / p.w.splits, split = blockIdx.x % p.w.splits;
   const int64_t r = p.r0 + row_i;
-  constexpr int kVec = CatRow<T>::kVec;
   griddep_enter();
   CatState* st = p.w.state + row_i;
   const int mode = st->mode;
@@ -1186,74 +1312,9 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_
     cat_search(sh, p, r, row, seg, q, by_k, sc, m);
     return;
   }
-  const float ta = st->ta, tb = st->tb, tk = st->tk, te = st->te;
-  const bool apart = st->apart != 0, upto = st->upto != 0;
   const int p0 = split * p.w.share, p1 = min(p0 + p.w.share, row.pieces());
-  u64 w_upto = 0, w_above, none = 0;
-  if (upto && !apart && sc.base == 0.0f) {
-    // top-p without top-k, the common case: every token's weight is wanted
-    w_above = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
-      u64 above = 0;
-      bool list = false;
-#pragma unroll
-      for (int h = 0; h < kVec; h += 4) {   // four exponentials side by side
-        float t[4];
-        u64 x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { t[i] = __fmul_rn(l[h + i], q.inv_t); x[i] = cat_bits(sc.exp0(t[i], sh.tab)); }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w_upto += x[i];
-          if (t[i] >= ta) above += x[i] - kCat256;
-          list = list || (t[i] >= tb && !(t[i] >= ta));
-        }
-        w_upto -= 4 * kCat256;
-      }
-      if (list) {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-          const float t = __fmul_rn(l[i], q.inv_t);
-          if (t >= tb && !(t >= ta)) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
-        }
-      }
-      return above;
-    });
-  } else {
-    const float need = upto ? tk : ta;
-    w_above = cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
-      u64 above = 0;
-      bool list = false;
-#pragma unroll
-      for (int h = 0; h < kVec; h += 4) {
-        float t[4];
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          t[i] = __fmul_rn(l[h + i], q.inv_t);
-          any = any || t[i] >= need || (upto && !apart);
-          list = list || (t[i] >= tb && !(t[i] >= ta)) || (apart && t[i] >= te && !(t[i] >= tk));
-        }
-        if (!__any_sync(0xffffffffu, any)) continue;
-        u64 x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = cat_bits(sc.exp(t[i], sh.tab)) - kCat256;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (t[i] >= ta) above += x[i];
-          if (upto && (!apart || t[i] >= tk)) w_upto += x[i];
-        }
-      }
-      if (list) {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-          const float t = __fmul_rn(l[i], q.inv_t);
-          if ((t >= tb && !(t >= ta)) || (apart && t >= te && !(t >= tk))) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
-        }
-      }
-      return above;
-    });
-  }
-  cat_reduce(sh, w_above, w_upto, none);
+  u64 w_upto = 0, none = 0, w_above = cat_weights<NT>(sh, row, p0, p1, seg, q, sc, m, *st, w_upto);
+  cat_reduce<NT>(sh, w_above, w_upto, none);
   u64* tot = p.w.tot + static_cast<int64_t>(row_i) * p.w.splits * 3;
   if (tid == 0) { __stcg(tot + split * 3, w_above); __stcg(tot + split * 3 + 1, w_upto); }
   u64* list = p.w.list + static_cast<int64_t>(row_i) * kCatList;
@@ -1261,7 +1322,7 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_
   if (!cat_last(sh, &st->ticket[1], p.w.splits)) return;
   w_above = 0; w_upto = 0;
   for (int i = tid; i < p.w.splits; i += kCatThreads) { w_above += __ldcg(tot + i * 3); w_upto += __ldcg(tot + i * 3 + 1); }
-  cat_reduce(sh, w_above, w_upto, none);
+  cat_reduce<NT>(sh, w_above, w_upto, none);
   CatCut x{};
   CatKept kept{};
   x.n = cat_get_list(sh, st, list, p.w.splits);
@@ -1269,6 +1330,152 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_
   x.by_k = by_k; x.by_p = q.by_p; x.apart = st->apart != 0; x.ends = st->ends != 0; x.k = q.want; x.top_p = q.top_p; x.least = cat_least(p, r, m);
   if (x.n <= kCatList && cat_resolve(sh, x, sc, kept)) cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
   else cat_search(sh, p, r, row, seg, q, by_k, sc, m);
+}
+
+// A row that fits shared memory, by one block: read once, every step without another kernel or another block to wait for.  NB threads pass
+// over the row, the first kCatThreads draw the conclusions.
+__host__ __device__ constexpr size_t cat_row_fixed() { return (sizeof(CatShared<kCatThreads>) + 15) / 16 * 16; }
+template <typename T, int NB>
+__global__ void __launch_bounds__(NB, 1024 / NB) cat_row_kernel(const __grid_constant__ CatParams p) {
+  extern __shared__ __align__(16) uint8_t cat_dyn[];
+  constexpr int NT = kCatThreads;
+  CatShared<NT>& sh = *reinterpret_cast<CatShared<NT>*>(cat_dyn);
+  u64* const seg = reinterpret_cast<u64*>(cat_dyn + cat_row_fixed());
+  uint4* const data = reinterpret_cast<uint4*>(seg + (p.w.pieces + 1) / 2 * 2);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t r = p.r0 + blockIdx.x;
+  constexpr int kVec = CatRow<T>::kVec, kU = NB >= 1024 ? 4 : 8;
+  griddep_enter();
+  const CatRequest q(p, r);
+  const CatRow<T> from(p.logits, r, p.V);
+  const CatHeld<T> row{data, from.head, p.V, (from.head + p.V + kVec - 1) / kVec};
+  cat_table(sh.tab);
+  if (tid == 0) sh.list_n = 0;
+  if (tid < NT) sh.rank[tid] = 0;
+  float mine = -INFINITY;
+  uint32_t live = 0;
+  for (int v0 = tid; v0 < row.vecs; v0 += kU * NB) {
+    uint4 raw[kU];
+#pragma unroll
+    for (int j = 0; j < kU; ++j) if (from.whole(v0 + j * NB)) raw[j] = from.vec(v0 + j * NB);
+#pragma unroll
+    for (int j = 0; j < kU; ++j) {
+      const int v = v0 + j * NB;
+      if (v >= row.vecs) break;
+      if (!from.whole(v)) raw[j] = from.edge(v);
+      data[v] = raw[j];
+      float l[kVec];
+      CatType<T>::unpack(raw[j], l);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) { mine = fmaxf(mine, l[i]); live += l[i] > -INFINITY; }
+    }
+  }
+  const uint32_t own = cat_ord(mine);
+  uint32_t top = __reduce_min_sync(0xffffffffu, own), low = __reduce_max_sync(0xffffffffu, mine > -INFINITY ? own : 0u);
+  live = __reduce_add_sync(0xffffffffu, live);
+  if (lane == 0) { sh.red[warp][0] = (static_cast<u64>(top) << 32) | live; sh.red[warp][1] = low; }
+  __syncthreads();
+  {
+    const u64 x = lane < NB / 32 ? sh.red[lane][0] : 0xffffffffull << 32;
+    top = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(x >> 32));
+    live = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(x));
+    low = __reduce_max_sync(0xffffffffu, lane < NB / 32 ? static_cast<uint32_t>(sh.red[lane][1]) : 0u);
+  }
+  if (live == 0) {   // nothing is left
+    if (tid == 0) {
+      if (p.dist) { double* d = p.dist + r * kCatRow; d[0] = -INFINITY; d[1] = INFINITY; d[2] = -1.0; d[3] = 0.0; d[4] = q.inv_t; }
+      if (p.u) { p.token[r] = -1; if (p.logp) p.logp[r] = -INFINITY; }
+    }
+    return;
+  }
+  const float raw_m = cat_key_value(static_cast<u64>(top) << 32), m = cat_scale(raw_m, q.inv_t);
+  const bool by_k = q.want > 0 && static_cast<uint32_t>(q.want) < live;
+  const int pieces = row.pieces();
+  const CatScale sc(m, kCatFloor);
+  CatKept kept{};
+  if (!by_k && !q.by_p) {
+    const float least = cat_least(p, r, m);
+    u64 w = cat_keep<NB>(row, 0, pieces, seg, q.inv_t, sc, sh.tab, least > -INFINITY ? CatBound{least, INT_MAX} : CatBound{-INFINITY, INT_MIN}, kept.n, kept.last);
+    cat_reduce<NB>(sh, w, kept.n, kept.last);
+    if (tid >= NT) return;
+    kept.w = w;
+    cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
+    return;
+  }
+  CatCut x{};
+  x.by_k = by_k; x.by_p = q.by_p; x.k = q.want; x.top_p = q.top_p;
+  const float width = raw_m - cat_key_value(static_cast<u64>(low) << 32);
+  if (by_k && q.few && width < 1e30f) {   // (no infinity among the logits)
+    // A threshold above which so many tokens lie for certain, by the threads' own maxima: these in buckets of equal width; the tokens
+    // of the buckets that hold that many maxima are listed.
+    const float scale = fminf(__fdividef(NT - 1.0f, fmaxf(width, 1e-30f)), FLT_MAX);
+    auto bucket = [&](float l) { return fminf((raw_m - l) * scale, static_cast<float>(NT)); };   // (masked: NT, the NaN of infinities too)
+    if (mine > -INFINITY) atomicAdd(&sh.rank[min(__float2uint_rd(bucket(mine)), NT - 1u)], 1u);
+    __syncthreads();
+    if (warp == 0) {
+      constexpr int kOwn = NT / 32;
+      uint32_t c[kOwn], sum = 0;
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) { c[j] = sh.rank[lane * kOwn + j]; sum += c[j]; }
+      uint32_t before = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, before, o); if (lane >= o) before += y; }
+      const uint32_t all = __shfl_sync(0xffffffffu, before, 31), want = static_cast<uint32_t>(q.want);
+      if (lane == 0 && all < want) sh.found_a = -1;
+      before -= sum;
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) { if (before < want && before + c[j] >= want) sh.found_a = lane * kOwn + j; before += c[j]; }
+    }
+    __syncthreads();
+    const int bucket_k = sh.found_a;
+    if (bucket_k >= 0) {
+      const float upto = static_cast<float>(bucket_k + 1);
+      cat_each<NB>(row, 0, pieces, [&](const float* l, int idx) {
+        float big = l[0];
+#pragma unroll
+        for (int i = 1; i < kVec; ++i) big = fmaxf(big, l[i]);
+        if (bucket(big) < upto) {
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) if (l[i] > -INFINITY && bucket(l[i]) < upto) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+        }
+      });
+      __syncthreads();
+      x.n = x.n1 = static_cast<int>(min(sh.list_n, kCatList + 1u));
+      if (x.n <= kCatList) {
+        if (tid >= NT) return;
+        x.least = cat_least(p, r, m);
+        if (cat_resolve(sh, x, sc, kept)) cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
+        else cat_search(sh, p, r, row, seg, q, by_k, sc, m);
+        return;
+      }
+      __syncthreads();
+      if (tid == 0) sh.list_n = 0;
+    }
+  }
+  {
+    constexpr int kEach = kCatBins / NB;
+    uint32_t n[kEach], f[kEach];
+    cat_count<NB>(sh, row, 0, pieces, q, m, n, f);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) { sh.hist[tid * kEach + j] = n[j]; sh.hist[kCatBins + tid * kEach + j] = f[j]; }
+    __syncthreads();
+    if (tid < NT) cat_bins<true>(sh, sh.hist, &sh.state, q, live, m, cat_least(p, r, m));
+    __syncthreads();
+  }
+  const CatState& st = sh.state;
+  if (st.mode == CAT_RANGE) {
+    u64 w_upto = 0, none = 0, w_above = cat_weights<NB>(sh, row, 0, pieces, seg, q, sc, m, st, w_upto);
+    cat_reduce<NB>(sh, w_above, w_upto, none);
+    if (tid >= NT) return;
+    x.n = static_cast<int>(min(sh.list_n, kCatList + 1u));
+    x.n1 = static_cast<int>(st.n1); x.n_above = st.at_a; x.n_mid = st.n_mid; x.w_above = w_above; x.w_upto = w_upto;
+    x.apart = st.apart != 0; x.ends = st.ends != 0; x.least = cat_least(p, r, m);
+    if (x.n <= kCatList && cat_resolve(sh, x, sc, kept)) {
+      cat_finish(sh, p, r, row, seg, q.inv_t, sc, m, kept);
+      return;
+    }
+  }
+  if (tid < NT) cat_search(sh, p, r, row, seg, q, by_k, sc, m);
 }
 
 // ------------------------------------------------------------------------------------------------------- verification
@@ -1334,7 +1541,8 @@ struct CatResampleParams {
 // integer sums by piece over (sequence, part of the row); the last block of a sequence finds the token.
 template <typename TQ, typename TP>
 __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __grid_constant__ CatResampleParams p) {
-  __shared__ CatShared sh;
+  __shared__ CatShared<kCatThreads> sh;
+  constexpr int NT = kCatThreads;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i_b = blockIdx.x / p.splits, split = blockIdx.x % p.splits, b = p.b0 + i_b;
   griddep_enter();
   cat_table(sh.tab);
@@ -1422,7 +1630,7 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
       }
       return all;
     }
-    return cat_sums(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
+    return cat_sums<NT>(row, p0, p1, seg, [&](const float* l, int idx) -> u64 {
       float y[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) y[i] = minus && idx + i >= 0 && idx + i < p.V ? cat_float(qrow.base[qrow.head + idx + i]) : -INFINITY;
@@ -1431,7 +1639,7 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
   };
   const int p0 = split * p.share, p1 = min(p0 + p.share, row.pieces());
   u64 total = pass(p0, p1, residual), none = 0, none2 = 0;
-  cat_reduce(sh, total, none, none2);
+  cat_reduce<NT>(sh, total, none, none2);
   u64* tot = p.tot + static_cast<int64_t>(i_b) * p.splits;
   if (tid == 0) __stcg(tot + split, total);
   uint32_t* ticket = &p.state[i_b].ticket[0];
@@ -1439,12 +1647,12 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
   if (tid == 0) *ticket = 0;                // for the next call
   total = 0;
   for (int i = tid; i < p.splits; i += kCatThreads) total += __ldcg(tot + i);
-  cat_reduce(sh, total, none, none2);
+  cat_reduce<NT>(sh, total, none, none2);
   bool minus = residual;
   if (total == 0 && minus) {                // p = q as far as 2^-52 goes: of p, by this block alone
     minus = false;
     total = pass(0, row.pieces(), false);
-    cat_reduce(sh, total, none, none2);
+    cat_reduce<NT>(sh, total, none, none2);
     __threadfence();
   }
   if (total == 0) return;

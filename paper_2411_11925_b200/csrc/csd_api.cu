@@ -1487,11 +1487,38 @@ void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int
   *splits = (*pieces + *share - 1) / *share;
 }
 
+// Rows that one block can hold: shared memory that takes, 0 where it does not fit.
+template <int NT>
+size_t cat_row_bytes(int V, int size, int pieces) {
+  const size_t bytes = cat_row_fixed() + static_cast<size_t>((pieces + 1) / 2 * 2) * 8 + (static_cast<size_t>(V) * size + 30) / 16 * 16;
+  return bytes <= (NT == 1024 ? 227 : 56) * 1024 ? bytes : 0;
+}
+template <typename T, int NT>
+int launch_cat_row(csd_ctx* ctx, const CatParams& p, int64_t rows, size_t smem) {
+  auto kern = cat_row_kernel<T, NT>;
+  static bool attr_done[kMaxDevices] = {};   // function attributes are per device
+  if (!attr_done[ctx->device]) {
+    CSD_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+    attr_done[ctx->device] = true;
+  }
+  return launch_short(ctx, ctx->stream, kern, static_cast<unsigned>(rows), NT, smem, p);
+}
+template <int NT>
+int launch_cat_row(csd_ctx* ctx, int dtype, const CatParams& p, int64_t rows, size_t smem) {
+  return dtype == CSD_F32 ? launch_cat_row<float, NT>(ctx, p, rows, smem) : dtype == CSD_BF16 ? launch_cat_row<__nv_bfloat16, NT>(ctx, p, rows, smem)
+                                                                                             : launch_cat_row<__half, NT>(ctx, p, rows, smem);
+}
+
 int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_cat_params* f, const float* u, int32_t* token, float* logp, double* dist) {
   CatParams p{};
   p.V = V; p.logits = CatView{l->data, l->ld};
   if (f) { p.temperature = f->temperature; p.top_k = f->top_k; p.top_p = f->top_p; p.min_p = f->min_p; }
   p.u = u; p.token = token; p.logp = logp; p.dist = dist;
+  const int size = l->dtype == CSD_F32 ? 4 : 2;
+  p.w.pieces = (V + 16 / size - 1 + kCatPiece - 1) / kCatPiece;
+  const size_t small = cat_row_bytes<256>(V, size, p.w.pieces), large = cat_row_bytes<1024>(V, size, p.w.pieces);
+  if (small && R > ctx->num_sms) return launch_cat_row<256>(ctx, l->dtype, p, R, small);
+  if (large && !getenv("CAT_SPLIT")) return launch_cat_row<1024>(ctx, l->dtype, p, R, large);
   // Rows go in groups whose workspace is bounded (32 KB a row).  Groups small enough for L2 to hold their logits from one kernel to
   // the next took longer: the passes are not bound by reading, and each group's kernels fill and drain the device once more (512 rows of
   // 131072 fp32 logits: GROUPFIG).

@@ -115,6 +115,29 @@ def test_wide_filters(V, k, p):
     ctx.close()
 
 
+def test_bins_that_end_near_zero_and_small_top_k_with_infinities():
+    """Borders between bins, and the least logit of min-p, next to zero, where fp32 numbers lie dense; a threshold for a small top-k where a
+    logit is infinite or the logits span the whole range."""
+    rng = np.random.default_rng(77)
+    V = 4000
+    x = (1.5 * rng.standard_normal((40, V))).astype(np.float32)
+    x[5, 7] = np.inf
+    x[6, :10] = 3e38; x[6, 10:20] = -3e38
+    x[7] = np.float32(3.912023); x[7, 5:] = 1e-20 * rng.standard_normal(V - 5)
+    fs = [dict(temperature=1.0, top_k=int(rng.choice([3, 2000, 0, 255])), top_p=float(np.float32(rng.choice([0.95, 1.0]))), min_p=float(np.float32(rng.choice([0.0, 0.02])))) for _ in range(40)]
+    for i in (5, 6):
+        fs[i].update(top_k=17)
+    fs[7].update(top_k=0, min_p=float(np.float32(0.02)))
+    u = rng.random(40).astype(np.float32)
+    ctx = _ctx()
+    for R in (40, 400):     # few rows and many
+        xs, us, ff = np.tile(x, (R // 40, 1)), np.tile(u, R // 40), fs * (R // 40)
+        tok, lp, d = _sample(ctx, _dev(xs), _dev(us), _params(ff), R, V)
+        _check_rows(xs[:40], tok[:40], lp[:40], d[:40], us[:40], ff[:40])
+        assert np.array_equal(tok, np.tile(tok[:40], R // 40)) and np.array_equal(d, np.tile(d[:40], (R // 40, 1)))
+    ctx.close()
+
+
 def test_rows_that_decide_by_rules():
     """Masks and extremes: nothing left, one left, the type's lowest value, infinities, zero temperature, filters at their ends."""
     V = 600
