@@ -1429,14 +1429,15 @@ __global__ void __launch_bounds__(NB, 1024 / NB) cat_row_kernel(const __grid_con
     __syncthreads();
     const int bucket_k = sh.found_a;
     if (bucket_k >= 0) {
-      const float upto = static_cast<float>(bucket_k + 1);
+      // everything above the bucket's lower end, a little below where that is rounded to
+      const float span = __fdividef(static_cast<float>(bucket_k + 1), scale), at = raw_m - span - (span + fabsf(raw_m)) * 1e-6f;
       cat_each<NB>(row, 0, pieces, [&](const float* l, int idx) {
         float big = l[0];
 #pragma unroll
         for (int i = 1; i < kVec; ++i) big = fmaxf(big, l[i]);
-        if (bucket(big) < upto) {
+        if (big >= at) {
 #pragma unroll
-          for (int i = 0; i < kVec; ++i) if (l[i] > -INFINITY && bucket(l[i]) < upto) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
+          for (int i = 0; i < kVec; ++i) if (l[i] >= at) sh.append(cat_key(cat_scale(l[i], q.inv_t), idx + i));
         }
       });
       __syncthreads();
@@ -1570,26 +1571,50 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
   const CatRow<TP> row(p.p, rp, p.V);
   const CatRow<TQ> qrow(p.q, residual ? rq : 0, p.V);
   constexpr int kVec = CatRow<TP>::kVec;
-  // a vector's weight; y: the draft's logits of the same tokens
+  // a vector's weight; y: the draft's logits of the same tokens.  Where neither normaliser is so large that it needs CatScale's base, scaled
+  // logits need no bounds either; the tokens equal to a cut, for which the index decides, are looked for apart.
+  const bool plain = sp.base == 0.0f && sq.base == 0.0f;
   auto weights = [&](const float* x, const float* y, int idx, bool minus) -> u64 {
     u64 sum = 0;
 #pragma unroll
     for (int h = 0; h < kVec; h += 4) {     // four exponentials side by side
       double a[4];
-      bool in[4], any = false;
+      float t[4];
+      bool in[4], any = false, edge = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { in[i] = kept_p.kept(cat_scale(x[h + i], inv_p), idx + h + i); any = any || in[i]; }
+      for (int i = 0; i < 4; ++i) {
+        t[i] = __fmul_rn(x[h + i], inv_p);
+        in[i] = t[i] > kept_p.value;
+        edge = edge || t[i] == kept_p.value;
+        any = any || in[i];
+      }
+      if (edge || !plain) {
+        any = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { t[i] = cat_scale(x[h + i], inv_p); in[i] = kept_p.kept(t[i], idx + h + i); any = any || in[i]; }
+      }
       if (!__any_sync(0xffffffffu, any)) continue;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = sp.exp(__fmul_rn(x[h + i], inv_p), sh.tab);
+      for (int i = 0; i < 4; ++i) a[i] = plain ? sp.exp0(t[i], sh.tab) : sp.exp(t[i], sh.tab);
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[i] = in[i] ? a[i] : 0.0;
       if (minus) {
         double d[4];
+        edge = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = sq.exp(__fmul_rn(y[h + i], inv_q), sh.tab);
+        for (int i = 0; i < 4; ++i) {
+          t[i] = __fmul_rn(y[h + i], inv_q);
+          in[i] = t[i] > kept_q.value;
+          edge = edge || t[i] == kept_q.value;
+        }
+        if (edge || !plain) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] -= kept_q.kept(cat_scale(y[h + i], inv_q), idx + h + i) ? d[i] : 0.0;
+          for (int i = 0; i < 4; ++i) { t[i] = cat_scale(y[h + i], inv_q); in[i] = kept_q.kept(t[i], idx + h + i); }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = plain ? sq.exp0(t[i], sh.tab) : sq.exp(t[i], sh.tab);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] -= in[i] ? d[i] : 0.0;
       }
       // 1 added: the bits behind 1's are the value in units of 2^-52
 #pragma unroll

@@ -1491,7 +1491,7 @@ void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int
 template <int NT>
 size_t cat_row_bytes(int V, int size, int pieces) {
   const size_t bytes = cat_row_fixed() + static_cast<size_t>((pieces + 1) / 2 * 2) * 8 + (static_cast<size_t>(V) * size + 30) / 16 * 16;
-  return bytes <= (NT == 1024 ? 227 : 56) * 1024 ? bytes : 0;
+  return bytes <= (227 * NT / 1024 - (NT < 1024)) * 1024 ? bytes : 0;   // 1024 threads an SM
 }
 template <typename T, int NT>
 int launch_cat_row(csd_ctx* ctx, const CatParams& p, int64_t rows, size_t smem) {
@@ -1516,9 +1516,11 @@ int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_ca
   p.u = u; p.token = token; p.logp = logp; p.dist = dist;
   const int size = l->dtype == CSD_F32 ? 4 : 2;
   p.w.pieces = (V + 16 / size - 1 + kCatPiece - 1) / kCatPiece;
-  const size_t small = cat_row_bytes<256>(V, size, p.w.pieces), large = cat_row_bytes<1024>(V, size, p.w.pieces);
-  if (small && R > ctx->num_sms) return launch_cat_row<256>(ctx, l->dtype, p, R, small);
-  if (large && !getenv("CAT_SPLIT")) return launch_cat_row<1024>(ctx, l->dtype, p, R, large);
+  const size_t by256 = cat_row_bytes<256>(V, size, p.w.pieces), by512 = cat_row_bytes<512>(V, size, p.w.pieces), by1024 = cat_row_bytes<1024>(V, size, p.w.pieces);
+  // ROWRULE
+  if (R > ctx->num_sms && by256) return launch_cat_row<256>(ctx, l->dtype, p, R, by256);
+  if (R > ctx->num_sms && by512) return launch_cat_row<512>(ctx, l->dtype, p, R, by512);
+  if (by1024 && (R > 16 || V <= 40000)) return launch_cat_row<1024>(ctx, l->dtype, p, R, by1024);
   // Rows go in groups whose workspace is bounded (32 KB a row).  Groups small enough for L2 to hold their logits from one kernel to
   // the next took longer: the passes are not bound by reading, and each group's kernels fill and drain the device once more (512 rows of
   // 131072 fp32 logits: GROUPFIG).
