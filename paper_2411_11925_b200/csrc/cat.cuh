@@ -23,6 +23,8 @@
 #include <limits.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ptx.cuh"
 
 namespace csd {
@@ -1571,57 +1573,67 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
   const CatRow<TP> row(p.p, rp, p.V);
   const CatRow<TQ> qrow(p.q, residual ? rq : 0, p.V);
   constexpr int kVec = CatRow<TP>::kVec;
-  // a vector's weight; y: the draft's logits of the same tokens.  Where neither normaliser is so large that it needs CatScale's base, scaled
-  // logits need no bounds either; the tokens equal to a cut, for which the index decides, are looked for apart.
-  const bool plain = sp.base == 0.0f && sq.base == 0.0f;
-  auto weights = [&](const float* x, const float* y, int idx, bool minus) -> u64 {
+  // a vector's weight; y: the draft's logits of the same tokens.  PLAIN: neither normaliser is so large that it needs CatScale's base, and
+  // scaled logits need no bounds either.  The tokens equal to a cut, for which the index decides, are looked for apart; what is not kept gets
+  // the least exponent, whose probability rounds to 0.
+  auto weights = [&](auto plain, const float* x, const float* y, int idx, bool minus) -> u64 {
+    constexpr bool kPlain = decltype(plain)::value;
     u64 sum = 0;
 #pragma unroll
     for (int h = 0; h < kVec; h += 4) {     // four exponentials side by side
       double a[4];
       float t[4];
-      bool in[4], any = false, edge = false;
+      bool any = false, edge = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        t[i] = __fmul_rn(x[h + i], inv_p);
-        in[i] = t[i] > kept_p.value;
-        edge = edge || t[i] == kept_p.value;
-        any = any || in[i];
+        const float v = kPlain ? __fmul_rn(x[h + i], inv_p) : cat_scale(x[h + i], inv_p);
+        const bool in = v > kept_p.value;
+        edge = edge || v == kept_p.value;
+        any = any || in;
+        t[i] = in ? v : -INFINITY;
       }
-      if (edge || !plain) {
-        any = false;
+      if (edge) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { t[i] = cat_scale(x[h + i], inv_p); in[i] = kept_p.kept(t[i], idx + h + i); any = any || in[i]; }
+        for (int i = 0; i < 4; ++i) {
+          const float v = cat_scale(x[h + i], inv_p);
+          if (v == kept_p.value && idx + h + i <= kept_p.idx) { t[i] = v; any = true; }
+        }
       }
       if (!__any_sync(0xffffffffu, any)) continue;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = plain ? sp.exp0(t[i], sh.tab) : sp.exp(t[i], sh.tab);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = in[i] ? a[i] : 0.0;
+      for (int i = 0; i < 4; ++i) a[i] = kPlain ? sp.exp0(t[i], sh.tab) : sp.exp(t[i], sh.tab);
       if (minus) {
-        double d[4];
         edge = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          t[i] = __fmul_rn(y[h + i], inv_q);
-          in[i] = t[i] > kept_q.value;
-          edge = edge || t[i] == kept_q.value;
+          const float v = kPlain ? __fmul_rn(y[h + i], inv_q) : cat_scale(y[h + i], inv_q);
+          edge = edge || v == kept_q.value;
+          t[i] = v > kept_q.value ? v : -INFINITY;
         }
-        if (edge || !plain) {
+        if (edge) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { t[i] = cat_scale(y[h + i], inv_q); in[i] = kept_q.kept(t[i], idx + h + i); }
+          for (int i = 0; i < 4; ++i) {
+            const float v = cat_scale(y[h + i], inv_q);
+            if (v == kept_q.value && idx + h + i <= kept_q.idx) t[i] = v;
+          }
         }
+        double d[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = plain ? sq.exp0(t[i], sh.tab) : sq.exp(t[i], sh.tab);
+        for (int i = 0; i < 4; ++i) d[i] = kPlain ? sq.exp0(t[i], sh.tab) : sq.exp(t[i], sh.tab);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] -= in[i] ? d[i] : 0.0;
+        for (int i = 0; i < 4; ++i) a[i] -= d[i];
       }
-      // 1 added: the bits behind 1's are the value in units of 2^-52
+      // 1 added: the bits behind 1's are the value in units of 2^-52; below 1's bits it was negative
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum += static_cast<u64>(__double_as_longlong(fmax(a[i], 0.0) + 1.0));
-      sum -= 4 * 0x3ff0000000000000ull;
+      for (int i = 0; i < 4; ++i) {
+        const long long bits = __double_as_longlong(a[i] + 1.0) - 0x3ff0000000000000ll;
+        sum += bits > 0 ? static_cast<u64>(bits) : 0;
+      }
     }
     return sum;
+  };
+  auto weights_of = [&](const float* x, const float* y, int idx, bool minus) {
+    return sp.base == 0.0f && sq.base == 0.0f ? weights(std::true_type(), x, y, idx, minus) : weights(std::false_type(), x, y, idx, minus);
   };
   // sums of pieces [p0, p1); this thread's own
   u64* seg = p.seg + static_cast<int64_t>(i_b) * p.pieces;
@@ -1646,7 +1658,7 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
             float x[kVec], y[CatRow<TQ>::kVec > kVec ? CatRow<TQ>::kVec : kVec];
             CatType<TP>::unpack(a[j], x);
             CatType<TQ>::unpack(d[j], y);
-            sum += weights(x, y, v * kVec - row.head, true);
+            sum += weights_of(x, y, v * kVec - row.head, true);
           }
         }
         all += sum;
@@ -1659,7 +1671,7 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
       float y[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) y[i] = minus && idx + i >= 0 && idx + i < p.V ? cat_float(qrow.base[qrow.head + idx + i]) : -INFINITY;
-      return weights(l, y, idx, minus);
+      return weights_of(l, y, idx, minus);
     });
   };
   const int p0 = split * p.share, p1 = min(p0 + p.share, row.pieces());
