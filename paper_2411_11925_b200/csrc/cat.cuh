@@ -11,10 +11,14 @@
 // integer sums do not depend on the order, so a cut or a token does not depend on how a row is spread over blocks, and a
 // prefix sum is off by 2^-42 of itself and 2^-45 a token: which of 10^5 tokens straddles top_p or u is decided as in 64-bit arithmetic.
 //
-// Three kernels, each over (row, part of the row): the largest logit (cat_top_kernel); counts by distance from it, or what needs no
+// A row that fits shared memory goes by one block (cat_row_kernel), which reads it once and does the passes there.  Other rows, and few long
+// ones, by three kernels over (row, part of the row): the largest logit (cat_top_kernel); counts by distance from it, or what needs no
 // counts (cat_scan_kernel); weights and the few candidates for the cut (cat_range_kernel).  The last block of a row to arrive draws the
 // conclusion for the row.  One kernel that kept a row in a cluster took 2 to 4 times as long: its passes shared 64 registers with
 // everything a row's state needs, and a reduction through distributed shared memory cost 1.3 us.
+//
+// Bound by instructions, not by reading: 52 a token with its weight (11 of them fp64), 24 a token counted.  512 rows of 131072 fp32 with top-p take
+// 303 us (the three kernels 47, 104 and 160; reading once at the copy rate 41), 576 of 65536 bf16 with top-k and top-p 71 (reading 12).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -224,12 +228,15 @@ __device__ __forceinline__ double cat_exp(float t, double c, const double* tab) 
   p = fma(p, r, l * l * l / 6);
   p = fma(p, r, l * l / 2);
   p = fma(p, r, l);
-  const double b = tab[k & 15];
-  const double v = fma(b * r, p, b);
-  return __hiloint2double(__double2hiint(v) + ((k >> 4) << 20), __double2loint(v));
+  const double e = tab[k & 15];   // 2^(j/16) less j in units of the exponent / 16: adding k there leaves its whole part
+  const double b = __hiloint2double(__double2hiint(e) + (k << 16), __double2loint(e));
+  return fma(b * r, p, b);
 }
 __device__ __forceinline__ void cat_table(double* tab) {
-  if (threadIdx.x < 16) tab[threadIdx.x] = exp2(threadIdx.x / 16.0);
+  if (threadIdx.x < 16) {
+    const double e = exp2(threadIdx.x / 16.0);
+    tab[threadIdx.x] = __hiloint2double(__double2hiint(e) - static_cast<int>(threadIdx.x << 16), __double2loint(e));
+  }
 }
 // exp(t - norm) of scaled logits t as 2^((t - base) log2(e) + c).  Where norm is so large that fp64 would lose what t - norm is, base
 // is the nearest fp32 number: t - base is exact for every t that matters (within a factor of two of base).  What lies more
@@ -926,7 +933,7 @@ __device__ __noinline__ void cat_search(CatShared<NT>& sh, const CatParams& p, i
 // ------------------------------------------------------------------------------------------------------------- kernels
 // The largest logit of a part (scaling is monotonic: the largest scaled one is its scaled logit) and how many are not masked; for a
 // small top-k also a threshold above which that many tokens of the row lie for certain: this part's share of them, by its threads' own maxima.
-// Bound by reading the logits.
+// Bound by reading the logits (512 x 131072 fp32 in 47 us, 5.7 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(kCatThreads) cat_top_kernel(const __grid_constant__ CatParams p) {
   __shared__ uint2 part[kCatWarps];
@@ -1153,14 +1160,14 @@ __device__ __forceinline__ u64 cat_weights(CatShared<TAIL>& sh, const R& row, in
         u64 x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) { t[i] = __fmul_rn(l[h + i], q.inv_t); x[i] = cat_bits(sc.exp0(t[i], sh.tab)); }
+        w_upto += x[0] + x[1] + x[2] + x[3] - 4 * kCat256;
+        if (!(m - fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) < db)) continue;   // few tokens make up most of a row's weight
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          w_upto += x[i];
           const float d = m - t[i];
           if (d < da) above += x[i] - kCat256;
           list = list || (d < db && !(d < da));
         }
-        w_upto -= 4 * kCat256;
       }
       if (list) {
 #pragma unroll
@@ -1290,7 +1297,8 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
 }
 
 // What cat_scan_kernel left: the weights above the bins in question (all weights where top-p refers to the whole row), piece by
-// piece, and the tokens of those bins, of which the row's last block derives the cut.  Bound by the exponentials: 4 cycles a warp of tokens in fp64.
+// piece, and the tokens of those bins, of which the row's last block derives the cut.  Bound by instructions:
+// 52 a token, two thirds of the issue slots taken, the fp64 pipe to 28 % (a third of the time is dependent fp64 steps at 32 warps an SM).
 template <typename T>
 __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_constant__ CatParams p) {
   __shared__ CatShared<kCatThreads> sh;

@@ -1477,13 +1477,14 @@ int check_cat_round(csd_ctx* ctx, int B, int gamma, int rows_p, int V) {
 
 CatView cat_view(const csd_logits* l) { return CatView{l->data, l->ld}; }
 
-// Parts of the rows: so many that `rows` of them give every SM sixteen blocks (four are resident), of 4096 to 32768 tokens each.
+// Parts of the rows: so many that `rows` of them give every SM sixteen blocks (four are resident), of 4096 to 65536 tokens each.
 void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int* splits, int* share, int* pieces) {
   const int size = l->dtype == CSD_F32 ? 4 : 2, vec = 16 / size;
   const bool aligned = reinterpret_cast<uintptr_t>(l->data) % 16 == 0 && (l->ld * size % 16 == 0 || rows == 1);
   *pieces = (V + (aligned ? 0 : vec - 1) + kCatPiece - 1) / kCatPiece;
   const int64_t want = (*pieces * rows + 16 * ctx->num_sms - 1) / (16 * ctx->num_sms);
-  *share = static_cast<int>(want < 8 ? 8 : want > 64 ? 64 : (want + 7) / 8 * 8);
+  const int least = static_cast<int>(want < 8 ? 8 : want > 64 ? 64 : want), parts = *pieces / least > 1 ? *pieces / least : 1;
+  *share = ((*pieces + parts - 1) / parts + 7) / 8 * 8;   // equal parts (512 rows of 131072 in 4 parts of 64 pieces 303 us, in 4 of 56 and one of 32 310)
   *splits = (*pieces + *share - 1) / *share;
 }
 
@@ -1517,13 +1518,16 @@ int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_ca
   const int size = l->dtype == CSD_F32 ? 4 : 2;
   p.w.pieces = (V + 16 / size - 1 + kCatPiece - 1) / kCatPiece;
   const size_t by256 = cat_row_bytes<256>(V, size, p.w.pieces), by512 = cat_row_bytes<512>(V, size, p.w.pieces), by1024 = cat_row_bytes<1024>(V, size, p.w.pieces);
-  // ROWRULE
+  // Rows that fit shared memory go by one block: 148 of 65536 bf16 with top-p 0.95 take 52 us, by the three kernels 113; 16 of 32768 with
+  // top-k 50 12.6 against 24.  With more rows than SMs two or four of them share an SM where they fit (600 rows of 16384 fp32, top-p: 68 us by 512
+  // threads, 91 by 1024).  Long rows in small numbers are left to many blocks: one of 90000 bf16 with top-p takes 61 us by one block, 40
+  // by many (top-k 50: 16 and 21); of 45000 fp32 35 and 32.
   if (R > ctx->num_sms && by256) return launch_cat_row<256>(ctx, l->dtype, p, R, by256);
   if (R > ctx->num_sms && by512) return launch_cat_row<512>(ctx, l->dtype, p, R, by512);
   if (by1024 && (R > 16 || V <= 40000)) return launch_cat_row<1024>(ctx, l->dtype, p, R, by1024);
   // Rows go in groups whose workspace is bounded (32 KB a row).  Groups small enough for L2 to hold their logits from one kernel to
   // the next took longer: the passes are not bound by reading, and each group's kernels fill and drain the device once more (512 rows of
-  // 131072 fp32 logits: GROUPFIG).
+  // 131072 fp32 logits with top-p 0.92: 512 us in groups of 64 MB, 332 in one).
   int64_t group = R < 1024 ? R : 1024;
   const int64_t groups = (R + group - 1) / group;
   group = (R + groups - 1) / groups;

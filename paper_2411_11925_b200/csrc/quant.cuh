@@ -154,7 +154,7 @@ __device__ __forceinline__ uint2 quant_pack8(const float* v, uint32_t byte) {
 template <typename T, int NCH> constexpr int quant_rows_resident() { return NCH == 1 || NCH == 2 ? 2 : 1; }
 
 // A block takes rows blockIdx.x, + gridDim.x, ...: the next row is requested before this one's reduction, so that its reads are under
-// way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, NORMFIG so; bound by
+// way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, 67 so; bound by
 // memory: 288 MB take 44 us at the rate of a copy).  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read
 // twice), 16 lanes a scale block.  Sums and the norm in fp32; the sum leaves rounded to the input's type, the norm uses it unrounded.
 template <typename T, int NCH, bool NORM>
