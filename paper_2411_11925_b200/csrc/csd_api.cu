@@ -1480,7 +1480,7 @@ CatView cat_view(const csd_logits* l) { return CatView{l->data, l->ld}; }
 // Parts of the rows: so many that `rows` of them give every SM sixteen blocks (four are resident), of 4096 to 65536 tokens each.
 void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int* splits, int* share, int* pieces) {
   const int size = l->dtype == CSD_F32 ? 4 : 2, vec = 16 / size;
-  const bool aligned = reinterpret_cast<uintptr_t>(l->data) % 16 == 0 && (l->ld * size % 16 == 0 || rows == 1);
+  const bool aligned = reinterpret_cast<uintptr_t>(l->data) % 16 == 0 && l->ld * size % 16 == 0;
   *pieces = (V + (aligned ? 0 : vec - 1) + kCatPiece - 1) / kCatPiece;
   const int64_t want = (*pieces * rows + 16 * ctx->num_sms - 1) / (16 * ctx->num_sms);
   const int least = static_cast<int>(want < 8 ? 8 : want > 64 ? 64 : want), parts = *pieces / least > 1 ? *pieces / least : 1;

@@ -329,6 +329,26 @@ def test_masked_target_rows_reject_and_give_no_token():
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_resampling_one_sequence_from_rows_off_16_bytes(dtype):
+    """A single sequence still reads a later row: its last tokens, which a row that starts on 16 bytes would not push into one more piece."""
+    gamma, V = 2, 4096
+    wide = torch.zeros(gamma + 1, V + 1, dtype=TYPES[dtype], device="cuda")
+    p = wide[:, :V]
+    p[:, V - 1] = 20.0
+    q = torch.zeros(gamma, V, dtype=TYPES[dtype], device="cuda")
+    ctx = _ctx()
+    dq, dp = (torch.zeros(r, 5, dtype=torch.float64, device="cuda") for r in (gamma, gamma + 1))
+    ctx.csd_cat_filter(gamma, V, q, None, dq)
+    ctx.csd_cat_filter(gamma + 1, V, p, None, dp)
+    for n in range(gamma + 1):
+        new = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+        ctx.csd_cat_resample(1, gamma, gamma + 1, V, q, dq, p, dp, torch.full_like(new, n), torch.full((1,), 0.5, device="cuda"), new)
+        ctx.sync()
+        assert int(new) == V - 1, n      # exp(20) against V - 1 ones: all but 1e-5 of the distribution
+    ctx.close()
+
+
 def test_bad_arguments_are_refused():
     from paper_2411_11925_b200 import api
     ctx = _ctx()
