@@ -1700,6 +1700,7 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
     cat_reduce<NT>(sh, total, none, none2);
     __threadfence();
   }
+  if (tid == 0) p.x_new[b] = -1;
   if (total == 0) return;
   const int found = cat_locate(sh, row, seg, cat_target(p.w[b], total), 0, [](u64) -> u64 { return 0; }, [&](const float* l, int idx, u64* w) {
 #pragma unroll

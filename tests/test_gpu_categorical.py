@@ -349,6 +349,22 @@ def test_resampling_one_sequence_from_rows_off_16_bytes(dtype):
     ctx.close()
 
 
+def test_summaries_that_give_no_weight_give_no_token():
+    V = 700
+    ctx = _ctx()
+    q, p = torch.zeros(1, V, device="cuda"), torch.zeros(2, V, device="cuda")
+    dq, dp = (torch.zeros(r, 5, dtype=torch.float64, device="cuda") for r in (1, 2))
+    ctx.csd_cat_filter(1, V, q, None, dq)
+    ctx.csd_cat_filter(2, V, p, None, dp)
+    dp[:, 0] = 1000.0                                # a normaliser that is not these rows'
+    for n in (0, 1):
+        new = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+        ctx.csd_cat_resample(1, 1, 2, V, q, dq, p, dp, torch.full_like(new, n), torch.full((1,), 0.5, device="cuda"), new)
+        ctx.sync()
+        assert int(new) == -1, n
+    ctx.close()
+
+
 def test_bad_arguments_are_refused():
     from paper_2411_11925_b200 import api
     ctx = _ctx()
