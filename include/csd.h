@@ -486,6 +486,8 @@ int csd_gmm_resample(csd_ctx *ctx, int B, int gamma, int C, int cap, const csd_g
  * tokens), the smallest scaled logit kept, the highest index kept among equals of it, the number of tokens kept, 1 / temperature.
  * Where every token is masked: -inf, inf, -1, 0.
  * Sums are 64-bit integers (weights to 2^-44 of the largest): results do not depend on how the work is spread over the device.
+ * The calls of a context share its workspace: they run on its stream, and a graph that holds one is not launched beside another call
+ * of the same context.  No output overlaps an input.
  *
  *   csd_cat_filter: dist of every row.
  *   csd_cat_draft_sample: the first token, in index order, whose cumulative probability reaches u[r] in (0,1); -1 where every token is
@@ -496,7 +498,7 @@ int csd_gmm_resample(csd_ctx *ctx, int B, int gamma, int C, int cap, const csd_g
  *     as csd_verify.  Equal logits and parameters give exactly 0.
  *   csd_cat_resample: x_new[b] = the token at position n_accept[b], w[b] in (0,1) its uniform: of max(0, p - q) for n_accept < gamma (of p
  *     where that is nothing), of p at the bonus position; -1 where n_accept = gamma and rows_p = gamma, where n_accept is
- *     outside [0, rows_p), and where p keeps nothing. */
+ *     outside [0, rows_p), and where p keeps nothing (or dist_p is not what csd_cat_verify wrote, and gives no token any weight). */
 typedef struct {
   const void *data;
   int dtype;
@@ -524,7 +526,7 @@ int csd_cat_resample(csd_ctx *ctx, int B, int gamma, int rows_p, int V, const cs
  *     under which its largest magnitude does not exceed 448; values are rounded to nearest even; a block with an infinity or a NaN becomes NaN.
  *   csd_norm_quantize: the same of h / sqrt(mean(h^2) + eps) * weight with h = x + residual (residual NULL: x; weight [K] of
  *     `dtype` or NULL: ones), formed in fp32.  sum [rows, K] of `dtype`, row stride lds, out or NULL: h, rounded; it may be x or
- *     residual itself (the residual stream is updated in place).
+ *     residual itself, rows at the same stride (the residual stream is updated in place), and overlaps them in no other way.
  *   csd_quant_matmul: out[m, n] = sum_k a[m, k] w[n, k], m < M token rows, n < N vocabulary rows, fp32 accumulation, rounded once to
  *     `dtype`; out DEVICE, row stride ldo.  Logits for the calls above. */
 typedef struct {

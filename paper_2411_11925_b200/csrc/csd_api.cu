@@ -1611,6 +1611,8 @@ int quant_rows(csd_ctx* ctx, int rows, int K, int dtype, QuantRowsParams p) {
   for (const void* a : {p.x, p.residual, p.weight, static_cast<const void*>(p.sum)})
     if (reinterpret_cast<uintptr_t>(a) % size) return fail(ctx, CSD_ERR_INVALID_ARG, "an array is not aligned to its type");
   if (p.ldx < 0 || p.ldr < 0 || (p.sum && rows > 1 && p.lds < K)) return fail(ctx, CSD_ERR_INVALID_ARG, "a row stride is negative, or the sum's rows overlap");
+  if (p.sum && rows > 1 && ((p.sum == p.x && p.lds != p.ldx) || (p.sum == p.residual && p.lds != p.ldr)))
+    return fail(ctx, CSD_ERR_INVALID_ARG, "the sum in place of an input has a row stride of its own");
   if (int rc = check_quant(ctx, p.data, p.scale, "the output")) return rc;
   csd_quant_pitch(K, &p.ld, &p.ls);
   p.K = K;

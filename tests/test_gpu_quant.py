@@ -203,6 +203,25 @@ def test_bad_arguments_are_refused():
     ctx.close()
 
 
+def test_sums_in_place_keep_their_rows():
+    """In place of an input only row on row: at another stride a row's sum would land where another block still reads."""
+    from paper_2411_11925_b200 import api
+    ctx = _ctx()
+    buf = torch.zeros(4 * 256, device="cuda")
+    x, tight = buf.view(4, 256)[:, :200], buf[:800].view(4, 200)
+    one = buf[:200].expand(4, -1)
+    q = _empty(4, 200)
+    other = torch.zeros(4, 200, device="cuda")
+    for a, r, s in ((x, None, tight), (one, None, tight), (other, x, tight), (other, one, tight)):
+        with pytest.raises(api.CsdError) as e:
+            ctx.csd_norm_quantize(4, 200, a, r, None, 1e-6, s, *q)
+        assert e.value.code == -1
+    ctx.csd_norm_quantize(4, 200, x, other, None, 1e-6, x, *q)
+    ctx.csd_norm_quantize(1, 200, x[:1], other[:1], None, 1e-6, tight[:1], q[0][:1], q[1][:1])   # a single row has no stride
+    ctx.sync()
+    ctx.close()
+
+
 def test_vocabulary_head_round_captured():
     """Norm, product, sampling, verification and resampling as one program, captured into a graph and replayed on new hidden states;
     each stage is checked against the plain form on the stage's own inputs."""
