@@ -188,7 +188,19 @@ __device__ __forceinline__ void cat_pieces(const R& row, int p0, int p1, F f, D 
   }
 }
 template <int NT, typename R, typename F>
-__device__ __forceinline__ void cat_each(const R& row, int p0, int p1, F f) { cat_pieces<NT>(row, p0, p1, f, [](int) {}); }
+__device__ __forceinline__ void cat_each(const R& row, int p0, int p1, F f) {
+  if constexpr (R::kShared) {   // vector by vector: few pieces keep all threads busy too
+    constexpr int kVec = R::kVec;
+#pragma unroll 2
+    for (int v = p0 * (kCatPiece / kVec) + threadIdx.x; v < min(p1 * (kCatPiece / kVec), row.vecs); v += NT) {
+      float l[kVec];
+      CatType<typename R::Type>::unpack(row.vec(v), l);
+      f(l, v * kVec - row.head);
+    }
+  } else {
+    cat_pieces<NT>(row, p0, p1, f, [](int) {});
+  }
+}
 // The same where f gives a vector's weight: the pieces' sums go to seg; returns this thread's own sum.
 template <int NT, typename R, typename F>
 __device__ __forceinline__ u64 cat_sums(const R& row, int p0, int p1, u64* seg, F f) {

@@ -1477,13 +1477,13 @@ int check_cat_round(csd_ctx* ctx, int B, int gamma, int rows_p, int V) {
 
 CatView cat_view(const csd_logits* l) { return CatView{l->data, l->ld}; }
 
-// Parts of the rows: so many that `rows` of them give every SM sixteen blocks (four are resident), of 4096 to 65536 tokens each.
-void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int* splits, int* share, int* pieces) {
+// Parts of the rows: so many that `rows` of them give every SM `blocks` of them (four are resident), of 4096 to `most` times 512 tokens each.
+void cat_parts(const csd_ctx* ctx, int64_t rows, const csd_logits* l, int V, int blocks, int most, int* splits, int* share, int* pieces) {
   const int size = l->dtype == CSD_F32 ? 4 : 2, vec = 16 / size;
   const bool aligned = reinterpret_cast<uintptr_t>(l->data) % 16 == 0 && l->ld * size % 16 == 0;
   *pieces = (V + (aligned ? 0 : vec - 1) + kCatPiece - 1) / kCatPiece;
-  const int64_t want = (*pieces * rows + 16 * ctx->num_sms - 1) / (16 * ctx->num_sms);
-  const int least = static_cast<int>(want < 8 ? 8 : want > 64 ? 64 : want), parts = *pieces / least > 1 ? *pieces / least : 1;
+  const int64_t want = (2 * blocks * ctx->num_sms + rows) / (2 * rows);
+  const int low = (*pieces + most - 1) / most, high = (*pieces + 7) / 8, parts = want < low ? low : want > high ? high : static_cast<int>(want);
   *share = ((*pieces + parts - 1) / parts + 7) / 8 * 8;   // equal parts (512 rows of 131072 in 4 parts of 64 pieces 303 us, in 4 of 56 and one of 32 310)
   *splits = (*pieces + *share - 1) / *share;
 }
@@ -1518,13 +1518,14 @@ int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_ca
   const int size = l->dtype == CSD_F32 ? 4 : 2;
   p.w.pieces = (V + 16 / size - 1 + kCatPiece - 1) / kCatPiece;
   const size_t by256 = cat_row_bytes<256>(V, size, p.w.pieces), by512 = cat_row_bytes<512>(V, size, p.w.pieces), by1024 = cat_row_bytes<1024>(V, size, p.w.pieces);
-  // Rows that fit shared memory go by one block: 148 of 65536 bf16 with top-p 0.95 take 52 us, by the three kernels 113; 16 of 32768 with
-  // top-k 50 12.6 against 24.  With more rows than SMs two or four of them share an SM where they fit (600 rows of 16384 fp32, top-p: 68 us by 512
-  // threads, 91 by 1024).  Long rows in small numbers are left to many blocks: one of 90000 bf16 with top-p takes 61 us by one block, 40
-  // by many (top-k 50: 16 and 21); of 45000 fp32 35 and 32.
+  // Rows that fit shared memory go by one block: 148 of 65536 bf16 with top-p 0.9 take 52 us, by the three kernels 73 (top-k 50: 16 and 28); 24 of
+  // 32768 30 and 37 (13 and 24).  More rows than SMs do where two or four fit an SM (600 of 32768 bf16: 102 us and 119, 41 and 43; of 16384 fp32
+  // 66 and 80, 37 and 37), so that one's dependent steps hide behind another's passes: one alone on an SM takes longer than the three kernels (300 of 65536: 124
+  // and 118, 40 and 37; 576: 194 and 187, 59 and 48).  Long rows in small numbers are left to many blocks: one of 90000 bf16 with top-p takes 61 us by
+  // one block, 40 by many (top-k 50: 16 and 21); of 45000 fp32 35 and 32.
   if (R > ctx->num_sms && by256) return launch_cat_row<256>(ctx, l->dtype, p, R, by256);
   if (R > ctx->num_sms && by512) return launch_cat_row<512>(ctx, l->dtype, p, R, by512);
-  if (by1024 && (R > 16 || V <= 40000)) return launch_cat_row<1024>(ctx, l->dtype, p, R, by1024);
+  if (by1024 && R <= ctx->num_sms && (R > 16 || V <= 40000)) return launch_cat_row<1024>(ctx, l->dtype, p, R, by1024);
   // Rows go in groups whose workspace is bounded (32 KB a row).  Groups small enough for L2 to hold their logits from one kernel to
   // the next took longer: the passes are not bound by reading, and each group's kernels fill and drain the device once more (512 rows of
   // 131072 fp32 logits with top-p 0.92: 512 us in groups of 64 MB, 332 in one).
@@ -1532,7 +1533,8 @@ int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_ca
   const int64_t groups = (R + group - 1) / group;
   group = (R + groups - 1) / groups;
   CatWork& w = p.w;
-  cat_parts(ctx, group, l, V, &w.splits, &w.share, &w.pieces);
+  // (one wave of blocks: each has a start and an end of dependent steps; 576 rows of 65536 in parts of 32 pieces 218 us, of 64 205, of 128 187)
+  cat_parts(ctx, group, l, V, 4, 128, &w.splits, &w.share, &w.pieces);
   const bool cuts = f && (f->top_k || f->top_p || f->temperature);   // (zero temperature keeps one token)
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
@@ -1562,7 +1564,8 @@ int cat_resample(csd_ctx* ctx, int B, int gamma, int rows_p, int V, const csd_lo
   p.gamma = gamma; p.rows = rows_p; p.V = V; p.q = CatView{q->data, q->ld}; p.p = CatView{l->data, l->ld};
   p.dist_q = dist_q; p.dist_p = dist_p; p.n_accept = n_accept; p.w = w; p.x_new = x_new;
   const int group = B < 4096 ? B : 4096;
-  cat_parts(ctx, group, l, V, &p.splits, &p.share, &p.pieces);
+  // (one pass, a short end: several waves even out better; 256 sequences of 131072 in parts of 32 pieces 107 us, of 64 113, of 128 124)
+  cat_parts(ctx, group, l, V, 16, 64, &p.splits, &p.share, &p.pieces);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
   const size_t g = static_cast<size_t>(group), o_seg = take(g * p.pieces * 8), o_tot = take(g * p.splits * 8);
