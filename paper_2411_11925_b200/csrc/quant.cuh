@@ -43,9 +43,15 @@ template <> __device__ __forceinline__ __half quant_from_float<__half>(float v) 
 // are read as aligned vectors too, one more than the elements fill, and shifted (element by element a warp's loads touch every line eight
 // times: 154 us against 117 at 8192 x 5001 bf16 with residual; fp32, 216 and 236, goes by element); so do not pieces that would reach beyond the row.
 template <typename T> struct QuantRaw { __align__(16) T e[8]; };
-template <typename T>
+// VEC: K is a multiple of 8 and rows are 16-byte aligned, a piece is a whole one or none.
+template <bool VEC, typename T>
 __device__ __forceinline__ void quant_load8(const T* row, int col, int K, QuantRaw<T>& v) {
   constexpr int kQ = sizeof(T) / 2;   // 16-byte vectors
+  if (VEC) {
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) reinterpret_cast<uint4*>(v.e)[i] = col < K ? reinterpret_cast<const uint4*>(row + col)[i] : make_uint4(0, 0, 0, 0);
+    return;
+  }
   const uintptr_t a = reinterpret_cast<uintptr_t>(row + col);
   const int off = static_cast<int>(a & 15);
   uint32_t* out = reinterpret_cast<uint32_t*>(v.e);
@@ -99,10 +105,15 @@ __device__ __forceinline__ void quant_round(const float* h, QuantRaw<__half>& v)
 #pragma unroll
   for (int i = 0; i < 4; ++i) reinterpret_cast<__half2*>(v.e)[i] = __floats2half2_rn(h[2 * i], h[2 * i + 1]);
 }
-template <typename T>
+template <bool VEC, typename T>
 __device__ __forceinline__ void quant_store8(T* row, int col, int K, const float* h) {
   QuantRaw<T> v;
   quant_round(h, v);
+  if (VEC) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) if (col < K) reinterpret_cast<uint4*>(row + col)[i] = reinterpret_cast<uint4*>(v.e)[i];
+    return;
+  }
   const uintptr_t a = reinterpret_cast<uintptr_t>(row + col);
   if ((a & 15) == 0 && col + 8 <= K) {
     constexpr int kQ = sizeof(T) / 2;
@@ -154,10 +165,10 @@ __device__ __forceinline__ uint2 quant_pack8(const float* v, uint32_t byte) {
 template <typename T, int NCH> constexpr int quant_rows_resident() { return NCH == 1 || NCH == 2 ? 2 : 1; }
 
 // A block takes rows blockIdx.x, + gridDim.x, ...: the next row is requested before this one's reduction, so that its reads are under
-// way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, 67 so; bound by
-// memory: 288 MB take 44 us at the rate of a copy).  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read
+// way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, 64 as it is;
+// 288 MB take 44 us at the rate of a copy, instructions bound 16-bit rows: 8192 x 4096 fp32 go at 6.4 TB/s, bf16 at 4.8).  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read
 // twice), 16 lanes a scale block.  Sums and the norm in fp32; the sum leaves rounded to the input's type, the norm uses it unrounded.
-template <typename T, int NCH, bool NORM>
+template <typename T, int NCH, bool NORM, bool VEC>
 __global__ void __launch_bounds__(NCH > 0 ? 512 : 1024, quant_rows_resident<T, NCH>()) quant_rows_kernel(const __grid_constant__ QuantRowsParams p) {
   __shared__ float part[2][32];
   constexpr int kN = NCH > 0 ? NCH : 1;
@@ -168,8 +179,8 @@ __global__ void __launch_bounds__(NCH > 0 ? 512 : 1024, quant_rows_resident<T, N
   auto row_r = [&](int64_t r) { return static_cast<const T*>(p.residual) + r * p.ldr; };
   QuantRaw<T> vx[kN], vr[kN];
   auto fetch = [&](int64_t r, int j, int c) {
-    quant_load8(row_x(r), c * 8, p.K, vx[j]);
-    if (p.residual) quant_load8(row_r(r), c * 8, p.K, vr[j]);
+    quant_load8<VEC>(row_x(r), c * 8, p.K, vx[j]);
+    if (p.residual) quant_load8<VEC>(row_r(r), c * 8, p.K, vr[j]);
   };
   auto take = [&](int j, float* h) {
     quant_floats(vx[j], h);
@@ -181,14 +192,14 @@ __global__ void __launch_bounds__(NCH > 0 ? 512 : 1024, quant_rows_resident<T, N
     }
   };
   auto put = [&](int64_t r, int c, float* h, float rstd) {   // (whole groups of 16 lanes are inside or outside)
-    if (p.sum) quant_store8(static_cast<T*>(p.sum) + r * p.lds, c * 8, p.K, h);
+    if (p.sum) quant_store8<VEC>(static_cast<T*>(p.sum) + r * p.lds, c * 8, p.K, h);
     if (NORM) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] *= rstd;
       if (wt) {
         QuantRaw<T> w;
         float y[8];
-        quant_load8(wt, c * 8, p.K, w);
+        quant_load8<VEC>(wt, c * 8, p.K, w);
         quant_floats(w, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] *= y[i];
