@@ -365,6 +365,29 @@ def test_summaries_that_give_no_weight_give_no_token():
     ctx.close()
 
 
+@pytest.mark.parametrize("R,V,k", [(3, 1000, 40), (3, 60001, 0)])
+def test_rows_beyond_32_bits(R, V, k):
+    """Row strides of 2^31 elements: the last row starts 2^32 elements and 2^33 bytes behind the first."""
+    rng = np.random.default_rng(V)
+    ctx = _ctx()
+    x = _dev((rng.standard_normal((R, V)) * 3).astype(np.float32), torch.bfloat16)
+    far = torch.empty((R - 1 << 31) + V, dtype=torch.bfloat16, device="cuda").as_strided((R, V), (1 << 31, 1))
+    far.copy_(x)
+    u = rng.random(R).astype(np.float32)
+    fs = [dict(temperature=0.8, top_k=k, top_p=0.9, min_p=0.0)] * R
+    a, b = _sample(ctx, far, _dev(u), _params(fs), R, V), _sample(ctx, x, _dev(u), _params(fs), R, V)
+    for i, j in zip(a, b):
+        assert np.array_equal(i, j)
+    q, new = torch.zeros(2, V, device="cuda"), [torch.full((1,), 9, dtype=torch.int32, device="cuda") for _ in range(2)]
+    dq, dp = torch.zeros(2, 5, dtype=torch.float64, device="cuda"), _dev(a[2])
+    ctx.csd_cat_filter(2, V, q, None, dq)
+    for l, o in ((far, new[0]), (x, new[1])):
+        ctx.csd_cat_resample(1, 2, 3, V, q, dq, l, dp, torch.full_like(o, 2), torch.full((1,), 0.3, device="cuda"), o)
+    ctx.sync()
+    assert int(new[0]) == int(new[1]) >= 0
+    ctx.close()
+
+
 def test_bad_arguments_are_refused():
     from paper_2411_11925_b200 import api
     ctx = _ctx()

@@ -222,6 +222,29 @@ def test_sums_in_place_keep_their_rows():
     ctx.close()
 
 
+def test_rows_beyond_32_bits():
+    """Row strides of 2^31 elements of inputs, of the sum and of a product's output."""
+    rows, K, N = 3, 200, 70
+    rng = np.random.default_rng(5)
+    ctx = _ctx()
+    x = torch.from_numpy(rng.standard_normal((rows, K)).astype(np.float32)).cuda().bfloat16()
+    far = torch.empty((rows - 1 << 31) + 256, dtype=torch.bfloat16, device="cuda")
+    fx, fo = far.as_strided((rows, K), (1 << 31, 1)), far.as_strided((rows, N), (1 << 31, 1))
+    fx.copy_(x)
+    near, other, sums = _empty(rows, K), _empty(rows, K), torch.empty_like(x)
+    ctx.csd_norm_quantize(rows, K, x, x, None, 1e-6, sums, *near)
+    ctx.csd_norm_quantize(rows, K, fx, x, None, 1e-6, fx, *other)
+    w = _quant(ctx, torch.from_numpy(rng.standard_normal((N, K)).astype(np.float32)).cuda())
+    ctx.sync()
+    assert torch.equal(near[0], other[0]) and torch.equal(near[1], other[1]) and torch.equal(fx, sums)
+    out = torch.empty(rows, N, dtype=torch.bfloat16, device="cuda")
+    ctx.csd_quant_matmul(rows, N, K, near, w, out)
+    ctx.csd_quant_matmul(rows, N, K, near, w, fo)
+    ctx.sync()
+    assert torch.equal(out, fo)
+    ctx.close()
+
+
 def test_vocabulary_head_round_captured():
     """Norm, product, sampling, verification and resampling as one program, captured into a graph and replayed on new hidden states;
     each stage is checked against the plain form on the stage's own inputs."""
