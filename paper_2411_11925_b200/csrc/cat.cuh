@@ -11,14 +11,14 @@
 // integer sums do not depend on the order, so a cut or a token does not depend on how a row is spread over blocks, and a
 // prefix sum is off by 2^-42 of itself and 2^-45 a token: which of 10^5 tokens straddles top_p or u is decided as in 64-bit arithmetic.
 //
-// A row that fits shared memory goes by one block (cat_row_kernel), which reads it once and does the passes there.  Other rows, and few long
-// ones, by three kernels over (row, part of the row): the largest logit (cat_top_kernel); counts by distance from it, or what needs no
+// A row that fits shared memory goes by one block (cat_row_kernel), which reads it once and does the passes there.  Other rows, few long ones and
+// many that would each fill an SM, by three kernels over (row, part of the row): the largest logit (cat_top_kernel); counts by distance from it, or what needs no
 // counts (cat_scan_kernel); weights and the few candidates for the cut (cat_range_kernel).  The last block of a row to arrive draws the
 // conclusion for the row.  One kernel that kept a row in a cluster took 2 to 4 times as long: its passes shared 64 registers with
 // everything a row's state needs, and a reduction through distributed shared memory cost 1.3 us.
 //
 // Bound by instructions, not by reading: 52 a token with its weight (11 of them fp64), 24 a token counted.  512 rows of 131072 fp32 with top-p take
-// 303 us (the three kernels 47, 104 and 160; reading once at the copy rate 41), 576 of 65536 bf16 with top-k and top-p 71 (reading 12).
+// 304 us (the three kernels 47, 104 and 160; reading once at the copy rate 41), 576 of 65536 bf16 with top-k 200 and top-p, with the ratios, 68 (reading 12).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
