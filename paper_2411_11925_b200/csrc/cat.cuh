@@ -872,7 +872,9 @@ __device__ __forceinline__ u64 cat_keep(const R& row, int p0, int p1, u64* seg, 
 template <int NT, typename R>
 __device__ __forceinline__ void cat_finish(CatShared<NT>& sh, const CatParams& p, int64_t r, const R& row, const u64* seg, float inv_t, const CatScale& sc, float m, const CatKept& kept) {
   const int tid = threadIdx.x;
-  const double norm = static_cast<double>(m) + log(static_cast<double>(kept.w)) - 44.0 * 0.69314718055994530942;
+  // The sum in units of the largest token's own weight: 2^44 but for the rounding of CatScale's c, which all weights share and the quotient takes
+  // out.  A token that is certain has the quotient 1, so the normaliser is its scaled logit and its log probability 0, exactly.
+  const double norm = static_cast<double>(m) + log(static_cast<double>(kept.w) / static_cast<double>(cat_weight(m, sc, sh.tab)));
   const CatBound bound{cat_key_value(kept.last), static_cast<int>(static_cast<uint32_t>(kept.last))};
   if (tid == 0 && p.dist) {
     double* d = p.dist + r * kCatRow;

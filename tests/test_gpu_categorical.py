@@ -454,3 +454,49 @@ def test_captured_calls_replay_on_new_inputs_and_other_streams():
     ctx.sync()
     del g
     ctx.close(); plain.close()
+
+
+@pytest.mark.parametrize("R,V,dtype", [(5, 1000, "f32"), (40, 30001, "bf16"), (300, 700, "f16"), (3, 100003, "f32"), (400, 33001, "f32")])
+def test_a_certain_token_has_log_probability_zero(R, V, dtype):
+    """One token kept, whatever leaves it alone and however large its logit: the normaliser is its scaled logit.  By one block a row (the first
+    three) and by the three kernels, with several parts a row and with one."""
+    rng = np.random.default_rng(V)
+    m = rng.uniform(-40, 60, R)
+    m[::3] = rng.uniform(60, 3000, m[::3].size)
+    x = (m[:, None] - rng.uniform(0.5, 20, (R, V))).astype(np.float32)
+    at = rng.integers(0, V, R)
+    x[np.arange(R), at] = m
+    l = _dev(x, TYPES[dtype])
+    x = _f32(l)
+    u = _dev(rng.random(R).astype(np.float32))
+    T = float(np.float32(0.7))
+    one = np.full_like(x, -np.inf)
+    one[np.arange(R), at] = x[np.arange(R), at]
+    ctx = _ctx()
+    for rows, f in ((x, dict(temperature=T, top_k=1)), (x, dict(temperature=0.0)), (x, dict(temperature=T, top_p=1e-6)), (x, dict(temperature=T, top_k=1, top_p=0.5)),
+                    (x, dict(temperature=T, min_p=1.0)), (one, dict(temperature=T)), (one, dict(temperature=T, top_p=0.9)), (one, dict(temperature=T, top_k=5))):
+        l = _dev(rows, TYPES[dtype])
+        tok, lp, d = _sample(ctx, l, u, _params([f] * R), R, V)
+        alone = d[:, 3] == 1          # (16-bit logits may have equals at the top)
+        assert alone.sum() > R / 2
+        assert np.all(lp[alone] == 0) and np.all(d[alone, 0] == d[alone, 1]), f
+        assert np.all(lp <= 0) and np.all(tok[alone] == d[alone, 2])
+    ctx.close()
+
+
+def test_certain_drafts_of_certain_targets_are_accepted():
+    """Greedy rows of p and q that keep the same token: the ratio is 0, and a uniform of 1 accepts."""
+    B, gamma, V = 50, 4, 2000
+    rng = np.random.default_rng(6)
+    p = (rng.standard_normal((B * gamma, V)) + rng.uniform(-40, 60, (B * gamma, 1))).astype(np.float32)
+    q = (p + rng.uniform(-3, 3, (B * gamma, 1))).astype(np.float32)
+    at = rng.integers(0, V, B * gamma)
+    for x in (p, q):
+        x[np.arange(B * gamma), at] += 10
+    greedy = _params([dict(temperature=0.0)] * (B * gamma))
+    u1 = torch.ones(B, gamma, device="cuda")
+    ctx = _ctx()
+    tok, dq, dp, lr, n, mask, new = _round(ctx, _dev(q), _dev(p), greedy, greedy, u1.view(-1), u1, u1[:, 0].contiguous(), B, gamma, gamma, V)
+    ctx.sync()
+    assert np.array_equal(tok.cpu().numpy().ravel(), at) and torch.all(lr == 0) and torch.all(n == gamma) and torch.all(mask == 15)
+    ctx.close()
