@@ -500,3 +500,46 @@ def test_certain_drafts_of_certain_targets_are_accepted():
     ctx.sync()
     assert np.array_equal(tok.cpu().numpy().ravel(), at) and torch.all(lr == 0) and torch.all(n == gamma) and torch.all(mask == 15)
     ctx.close()
+
+
+def _check_kept(x, d, fs):
+    for r in range(x.shape[0]):
+        row = _cat.kept(x[r], **fs[r])[2]
+        assert np.array_equal(d[r, 1:], row[1:]), (r, d[r], row, fs[r])
+
+
+@pytest.mark.parametrize("R,V", [(1, 1000), (60, 2000), (400, 33001), (3, 100003)])
+def test_equals_by_scaling_go_by_index(R, V):
+    """Different logits that scale to the same number are equals, of which the index decides: neighbours in the last bit, products beyond the range, and
+    products that are zero or next to it.  By one block a row (the first two), by the three kernels with one part a row and with several."""
+    ctx = _ctx()
+    u = _dev(np.full(R, 0.5, np.float32))
+    a, b = np.float32(1.75 + 2.0 ** -23), np.float32(1.75 + 2.0 ** -22)
+    assert a < b and a * np.float32(1.25) == b * np.float32(1.25)
+    near, big, flat = np.zeros((R, V), np.float32), np.zeros((R, V), np.float32), np.zeros((R, V), np.float32)
+    near[:, 0] = a; near[:, 4] = b
+    near[:, V - 1] = b; near[:, V // 2] = a
+    big[:, 3] = 4.0; big[:, 7] = 5.0; big[:, 9] = -np.inf; big[:, V - 5] = 6.0
+    flat[:, 1] = -np.inf; flat[:, 5:90] = 3.0; flat[:, V - 2] = 2.0
+    small = np.tile(np.float32(1.0) + np.arange(V, dtype=np.float32) * np.float32(2.0 ** -23), (R, 1))
+    for x, T in ((near, 0.8), (big, 2e-38), (flat, np.inf), (small, 1e38)):
+        for k in (1, 2, 3, 20, 200):
+            for p in (1.0, 0.7):
+                fs = [dict(temperature=float(np.float32(T)), top_k=k, top_p=p)] * R
+                _, _, d = _sample(ctx, _dev(x), u, _params(fs), R, V)
+                _check_kept(x[:1], d[:1], fs)
+                assert np.array_equal(d, np.repeat(d[:1], R, 0))
+    ctx.close()
+
+
+@pytest.mark.parametrize("R,V", [(400, 33001), (2, 100003), (30, 20000)])
+def test_small_top_k_of_large_logits(R, V):
+    """Logits of a million and a few units: many neighbours in the last bit, at temperatures that make equals of some of them."""
+    rng = np.random.default_rng(R)
+    ctx = _ctx()
+    for k in (1, 20, 50):
+        x = (1e6 + rng.standard_normal((R, V))).astype(np.float32)
+        fs = [dict(temperature=float(np.float32(rng.uniform(0.5, 1.3))), top_k=k) for _ in range(R)]
+        _, _, d = _sample(ctx, _dev(x), _dev(np.full(R, 0.5, np.float32)), _params(fs), R, V)
+        _check_kept(x, d, fs)
+    ctx.close()
