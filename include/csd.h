@@ -494,8 +494,8 @@ int csd_gmm_resample(csd_ctx *ctx, int B, int gamma, int C, int cap, const csd_g
  *     masked.  logp device [R] out or NULL: its log probability; dist out or NULL.
  *   csd_cat_verify: logits_q, dist_q, token [B, gamma] and u [B, gamma] of the drafts; logits_p [B, rows_p] rows with rows_p = gamma, or
  *     gamma + 1 where the bonus position is evaluated too; dist_p [B * rows_p, 5] out (all rows).  logratio = log p(x) - log q(x): -inf
- *     where x is not kept by p (or not in [0, V)), inf where it is kept by p only; accept iff log u <= logratio; n_accept, accept_mask
- *     as csd_verify.  Equal logits and parameters give exactly 0.
+ *     where x is not kept by p (or not in [0, V)), inf where it is kept by p only; u in [0,1]: accept iff log u <= logratio, never where that
+ *     is -inf; n_accept, accept_mask as csd_verify.  Equal logits and parameters give exactly 0.
  *   csd_cat_resample: x_new[b] = the token at position n_accept[b], w[b] in (0,1) its uniform: of max(0, p - q) for n_accept < gamma (of p
  *     where that is nothing), of p at the bonus position; -1 where n_accept = gamma and rows_p = gamma, where n_accept is
  *     outside [0, rows_p), and where p keeps nothing (or dist_p is not what csd_cat_verify wrote, and gives no token any weight). */

@@ -1526,7 +1526,7 @@ __device__ __forceinline__ double cat_log_prob(const CatView& m, int64_t row, co
   return kept ? static_cast<double>(t) - d[0] : -INFINITY;
 }
 
-// A warp per sequence, a lane per position: logratio = log p(x) - log q(x), accept iff log u <= logratio, n_accept = leading accepts.
+// A warp per sequence, a lane per position: logratio = log p(x) - log q(x), accept iff log u <= logratio and p keeps x, n_accept = leading accepts.
 template <typename TQ, typename TP>
 __global__ void __launch_bounds__(128) cat_verify_kernel(const CatVerifyParams p) {
   griddep_enter();
@@ -1542,7 +1542,7 @@ __global__ void __launch_bounds__(128) cat_verify_kernel(const CatVerifyParams p
       if (lp > -INFINITY) ratio = lq > -INFINITY ? lp - lq : INFINITY;
     }
     p.logratio[r] = static_cast<float>(ratio);
-    ok = log(static_cast<double>(p.u[r])) <= ratio;
+    ok = ratio > -INFINITY && log(static_cast<double>(p.u[r])) <= ratio;   // (a uniform of 0 accepts no token that p does not keep)
   }
   const uint32_t mask = __ballot_sync(0xffffffffu, ok);
   if (lane == 0) {

@@ -543,3 +543,26 @@ def test_small_top_k_of_large_logits(R, V):
         _, _, d = _sample(ctx, _dev(x), _dev(np.full(R, 0.5, np.float32)), _params(fs), R, V)
         _check_kept(x, d, fs)
     ctx.close()
+
+
+def test_a_uniform_of_zero_accepts_no_token_that_is_not_kept():
+    """log 0 is no larger than a ratio of -inf: tokens that p masks or filters out, and numbers that are no tokens, are rejected all the same."""
+    B, gamma, V = 6, 3, 300
+    rng = np.random.default_rng(13)
+    p = rng.standard_normal((B, gamma, V)).astype(np.float32)
+    tok = np.tile(np.array([5, 6, 7], np.int32), (B, 1))
+    p[:, :, 5:8] = 4.0
+    p[0, 1, 6] = -np.inf                      # masked by p
+    p[1, 0, 5] = -9.0                         # not among p's top-k
+    tok[2, 0], tok[3, 2], tok[4, 1] = -1, V, np.iinfo(np.int32).min
+    q = _dev(rng.standard_normal((B * gamma, V)).astype(np.float32))
+    f = lambda rows: _params([dict(top_k=9)] * rows)  # noqa: E731
+    dq, dp = (torch.zeros(B * gamma, 5, dtype=torch.float64, device="cuda") for _ in range(2))
+    lr, n, mask = torch.zeros(B, gamma, device="cuda"), torch.full((B,), 9, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    ctx = _ctx()
+    ctx.csd_cat_filter(B * gamma, V, q, None, dq)
+    for u in (0.0, 2.0 ** -149):
+        ctx.csd_cat_verify(B, gamma, gamma, V, q, dq, _dev(p.reshape(-1, V)), f(B * gamma), _dev(tok), torch.full((B, gamma), u, device="cuda"), dp, lr, n, mask)
+        ctx.sync()
+        assert n.tolist() == [1, 0, 0, 2, 1, 3] and mask.tolist() == [5, 6, 6, 3, 5, 7], u
+    ctx.close()
