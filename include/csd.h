@@ -498,7 +498,7 @@ int csd_gmm_resample(csd_ctx *ctx, int B, int gamma, int C, int cap, const csd_g
  *     is -inf; n_accept, accept_mask as csd_verify.  Equal logits and parameters give exactly 0.
  *   csd_cat_resample: x_new[b] = the token at position n_accept[b], w[b] in (0,1) its uniform: of max(0, p - q) for n_accept < gamma (of p
  *     where that is nothing), of p at the bonus position; -1 where n_accept = gamma and rows_p = gamma, where n_accept is
- *     outside [0, rows_p), and where p keeps nothing (or dist_p is not what csd_cat_verify wrote, and gives no token any weight). */
+ *     outside [0, rows_p), and where p keeps nothing.  With summaries that are not those of these rows it is -1 or some token of [0, V). */
 typedef struct {
   const void *data;
   int dtype;

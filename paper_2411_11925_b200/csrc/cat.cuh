@@ -541,7 +541,8 @@ __device__ __forceinline__ u64 cat_target(float u, u64 total) {
 
 // The token at which the cumulative weight reaches target, by one block: seg has the sums of all pieces, without the weights of
 // the first `extra` entries of the list (listed(key)); the piece that holds the token is gone through again, a warp a vector.
-// weights(l, idx, w): of a vector's logits, as in the pass that formed the sums, listed tokens included.  One thread gets the token, the others -1.
+// weights(l, idx, w): of a vector's logits, as in the pass that formed the sums, listed tokens included.  One thread gets the token, the others -1;
+// all get -1 where no piece reaches target.
 template <int NT, typename R, typename W, typename L>
 __device__ __forceinline__ int cat_locate(CatShared<NT>& sh, const R& row, const u64* seg, u64 target, int extra, L listed, W weights) {
   constexpr int kVec = R::kVec, kIts = kCatPiece / (32 * kVec), kEach = (kCatMaxPieces + NT - 1) / NT;
@@ -571,6 +572,7 @@ __device__ __forceinline__ int cat_locate(CatShared<NT>& sh, const R& row, const
     }
     s += x[j];
   }
+  if (tid == 0) sh.found_piece = -1;
   u64 before = cat_block_scan<NT, u64>(s, sh.scan, &total) - s;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
@@ -579,6 +581,7 @@ __device__ __forceinline__ int cat_locate(CatShared<NT>& sh, const R& row, const
   }
   cat_sync<NT>();
   const int piece = sh.found_piece;
+  if (piece < 0) return -1;   // sums beyond 64 bits: of a summary that is not this row's
   u64 w[kVec], incl = 0;
   int idx = 0;
   if (warp < kIts) {
@@ -1723,7 +1726,8 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_resample_kernel(const __gr
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       const float t = cat_scale(l[i], inv_p);
-      double a = kept_p.kept(t, idx + i) ? sp.exp(t, sh.tab) : 0.0;
+      const bool in = static_cast<unsigned>(idx + i) < static_cast<unsigned>(p.V);   // (a summary whose cut is -inf keeps what is masked: outside the row too)
+      double a = in && kept_p.kept(t, idx + i) ? sp.exp(t, sh.tab) : 0.0;
       if (minus && a > 0.0) {
         const float tq = cat_scale(cat_float(qrow.base[qrow.head + idx + i]), inv_q);
         if (kept_q.kept(tq, idx + i)) a -= sq.exp(tq, sh.tab);

@@ -566,3 +566,44 @@ def test_a_uniform_of_zero_accepts_no_token_that_is_not_kept():
         ctx.sync()
         assert n.tolist() == [1, 0, 0, 2, 1, 3] and mask.tolist() == [5, 6, 6, 3, 5, 7], u
     ctx.close()
+
+
+@pytest.mark.parametrize("V,tq,tp", [(701, "f32", "f32"), (5003, "bf16", "bf16"), (5003, "bf16", "f32")])
+def test_summaries_of_other_rows_give_some_token_or_none(V, tq, tp):
+    """Whatever the summaries say, the answer is -1 or a token, nothing outside the rows is read (they end where their memory does), and the next call is
+    right: normalisers far off either way, cuts of -inf, numbers that are none."""
+    B, gamma, nan, inf = 4, 2, np.nan, np.inf
+    rng = np.random.default_rng(V)
+    p, q = (_dev((rng.standard_normal((r, V)) * 2).astype(np.float32), TYPES[t]) for r, t in ((B * (gamma + 1), tp), (B * gamma, tq)))
+    dp, dq = torch.zeros(B * (gamma + 1), 5, dtype=torch.float64, device="cuda"), torch.zeros(B * gamma, 5, dtype=torch.float64, device="cuda")
+    n = torch.tensor([0, 1, 2, 0], dtype=torch.int32, device="cuda")
+    w = _dev(np.array([0.1, 0.5, 0.999, 1.0], np.float32))
+    ctx = _ctx()
+    ctx.csd_cat_filter(B * gamma, V, q, None, dq)
+    ctx.csd_cat_filter(B * (gamma + 1), V, p, None, dp)
+    right, new = torch.full((B,), 9, dtype=torch.int32, device="cuda"), torch.full((B,), 9, dtype=torch.int32, device="cuda")
+    ctx.csd_cat_resample(B, gamma, gamma + 1, V, q, dq, p, dp, n, w, right)
+    ctx.sync()
+    for col, values in ((0, (-30.0, -3000.0, -4000.0, -5000.0, -1e30, -1e300, 1e30, nan, inf, -inf)), (1, (-inf, nan, inf, -1e300)),
+                        (2, (nan, 1e300, -1e300, inf)), (3, (nan, 1e300, inf)), (4, (nan, inf, -1.0, 0.0, 1e30, -1e300))):
+        for v in values:
+            for both in (False, True):
+                fp, fq = dp.clone(), dq.clone()
+                fp[:, col] = v
+                if both:
+                    fq[:, col] = v
+                if col == 2:
+                    fp[:, 1] = -inf; fq[:, 1] = -inf
+                new.fill_(V)
+                ctx.csd_cat_resample(B, gamma, gamma + 1, V, q, fq, p, fp, n, w, new)
+                ctx.sync()
+                assert torch.all((new >= -1) & (new < V)), (col, v, both, new)
+    # a cut of -inf with every index is no cut
+    fp = dp.clone(); fp[:, 1] = -inf; fp[:, 2] = 1e9
+    ctx.csd_cat_resample(B, gamma, gamma + 1, V, q, dq, p, fp, n, w, new)
+    ctx.sync()
+    assert torch.equal(new, right)
+    ctx.csd_cat_resample(B, gamma, gamma + 1, V, q, dq, p, dp, n, w, new)
+    ctx.sync()
+    assert torch.equal(new, right)
+    ctx.close()
