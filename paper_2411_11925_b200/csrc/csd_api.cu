@@ -23,6 +23,7 @@
 #include "groupchain.cuh"
 #include "widechain.cuh"
 #include "f32chain.cuh"
+#include "hostio.h"
 #include "cat.cuh"
 #include "quant.cuh"
 
@@ -46,17 +47,12 @@ struct ChainWs {
   float* hid = nullptr; // hidden layer of the timestep embedding [T, W]
   bool owned = true;    // false: base is memory the library did not allocate and must never free or grow
   bool in_graph = false;
+  void drop() { base = nullptr; cap = 0; in_graph = false; }
 };
 
 constexpr int kMaxDevices = 64;   // device ordinals the per-device tables below cover
 
 struct ProfRec { cudaEvent_t a, b; int cls; double flops; };
-
-struct HostIo {  // a device buffer that grows on demand
-  void* base = nullptr;
-  size_t cap = 0;
-  bool in_graph = false;   // a captured call used it: its graph holds the address
-};
 
 }  // namespace
 
@@ -259,7 +255,7 @@ template <typename Buf>
 int give_up(csd_ctx* ctx, Buf& b) {
   void* const base = b.base;
   const bool keep = b.in_graph;
-  b.base = nullptr; b.cap = 0; b.in_graph = false;
+  b.drop();
   if (base && keep) ctx->in_graphs.push_back(base);
   else if (base) CSD_CUDA(ctx, cudaFree(base));
   return CSD_OK;
@@ -1571,9 +1567,8 @@ int cat_resample(csd_ctx* ctx, int B, int gamma, int rows_p, int V, const csd_lo
   const size_t g = static_cast<size_t>(group), o_seg = take(g * p.pieces * 8), o_tot = take(g * p.splits * 8);
   // the tickets lie at the buffer's start at their most, so that no call's sums ever take their place: they are zero between calls
   const size_t tickets = align_up(4096 * sizeof(CatState), 256);
-  const size_t had = ctx->cr.cap;
   if (int rc = ensure_buffer(ctx, ctx->cr, tickets + off, "the sums of resampling")) return rc;
-  if (ctx->cr.cap != had) CSD_CUDA(ctx, cudaMemsetAsync(ctx->cr.base, 0, tickets, ctx->stream));
+  if (int rc = clear_once(ctx->cr, capturing(ctx), [&]() -> int { CSD_CUDA(ctx, cudaMemsetAsync(ctx->cr.base, 0, tickets, ctx->stream)); return CSD_OK; })) return rc;
   char* b = static_cast<char*>(ctx->cr.base);
   p.state = reinterpret_cast<CatState*>(b);
   p.seg = reinterpret_cast<u64*>(b + tickets + o_seg); p.tot = reinterpret_cast<u64*>(b + tickets + o_tot);
