@@ -779,6 +779,7 @@ template <int NT>
 __device__ __noinline__ bool cat_resolve(CatShared<NT>& sh, const CatCut& x, const CatScale& sc, CatKept& out) {
   const int tid = threadIdx.x;
   constexpr int kEach = kCatList / NT;
+  if (x.n < x.n1) return false;               // (not what was counted)
   cat_sort(sh, x.n);
   // a thread holds `each` entries in a row
   const int each = x.n <= NT ? 1 : x.n <= 2 * NT ? 2 : kEach;
@@ -1125,8 +1126,9 @@ __device__ __noinline__ void cat_bins(CatShared<NT>& sh, const uint32_t* hist, C
     st->at_a = sh.at_a; st->n1 = sh.at_b - sh.at_a; st->n_mid = apart ? sh.at_k - sh.at_b : 0;
     st->apart = apart; st->upto = q.by_p && (apart || !by_k); st->ends = ends;
   }
-  // (a token lies in a bin before b iff its distance is below b / 64: the places are products by a power of two)
-  if (tid == 0) { st->da = bin_a / kCatPerUnit; st->db = (bin_b + 1) / kCatPerUnit; st->dk = bin_k / kCatPerUnit; st->de = (bin_k + 1) / kCatPerUnit; }
+  // (a token lies in a bin before b iff its distance is below b / 64: the places are products by a power of two; no token lies before bin 0, one
+  // scaled beyond the range neither, whose distance from the largest is -inf where it is not cut off)
+  if (tid == 0) { st->da = bin_a > 0 ? bin_a / kCatPerUnit : -INFINITY; st->db = (bin_b + 1) / kCatPerUnit; st->dk = bin_k / kCatPerUnit; st->de = (bin_k + 1) / kCatPerUnit; }
 }
 
 // Counts tokens of pieces [p0, p1) by distance from the largest, and adds up their places: for bins tid * kEach + j.  One addition a token: count and

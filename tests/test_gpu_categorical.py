@@ -607,3 +607,30 @@ def test_summaries_of_other_rows_give_some_token_or_none(V, tq, tp):
     ctx.sync()
     assert torch.equal(new, right)
     ctx.close()
+
+
+@pytest.mark.parametrize("R,V,dtype", [(2, 1000, "f32"), (30, 30001, "bf16"), (200, 20011, "f16"), (400, 33001, "f32"), (3, 100003, "f32")])
+def test_infinite_and_overflowing_logits_at_the_top(R, V, dtype):
+    """Logits that are infinite, or are once scaled, are the largest ones, equals by index: they are what every filter keeps first, and a greedy row's token."""
+    rng = np.random.default_rng(V)
+    base = (2 * rng.standard_normal((R, V))).astype(np.float32)
+    big = {"f32": 3e38, "bf16": 3e38, "f16": 6e4}[dtype]
+    few, many = base.copy(), base.copy()
+    few[:, V // 3] = np.inf
+    many[:, [V - 1, 17, V // 2]] = np.inf
+    many[:, 5] = big; many[:, 9] = -np.inf
+    ctx = _ctx()
+    u = _dev(rng.random(R).astype(np.float32))
+    for x in (few, many):
+        l = _dev(x, TYPES[dtype])
+        for f in (dict(temperature=0.0), dict(top_k=1), dict(top_k=2), dict(top_k=17), dict(top_k=300), dict(top_k=700, top_p=0.5), dict(top_k=1, top_p=0.9), dict(top_p=0.4),
+                  dict(top_p=0.9), dict(min_p=0.5), dict(top_k=2, min_p=0.5), dict(top_p=0.9, min_p=0.1), dict()):
+            for T in (1.0, 0.25):
+                g = {"temperature": T, **f}
+                tok, lp, d = _sample(ctx, l, u, _params([g] * R), R, V)
+                h = _f32(l[:1])
+                _check_rows(h, tok[:1], lp[:1], d[:1], u[:1].cpu().numpy(), [g])
+                assert np.all(np.isin(tok, [V // 3] if x is few else ([V - 1, 17, V // 2] + [5] * (T < 1 and dtype != "f16"))))
+                for r in rng.integers(0, R, 2):
+                    assert np.array_equal(d[r, 1:], _cat.kept(_f32(l[r:r + 1])[0], **g)[2][1:]), (r, g, d[r])
+    ctx.close()
