@@ -475,10 +475,9 @@ int csd_gmm_resample(csd_ctx *ctx, int B, int gamma, int C, int cap, const csd_g
  * position is drawn from it directly, with one uniform and no loop.
  *
  * csd_logits: data DEVICE [rows, V], row r at data + r * ld elements, any alignment of rows (0 <= ld); dtype CSD_F32, CSD_BF16 or
- * CSD_F16; V <= 2^19.  -inf and NaN mask a token; every other value is finite (the type's lowest value is an ordinary, very unlikely
- * logit; infinity counts as the largest finite fp32 number).
+ * CSD_F16; V <= 2^19.  -inf and NaN mask a token; every other value is a logit (the type's lowest value an ordinary, very unlikely one).
  * csd_cat_params: DEVICE arrays, one value a row, each or the whole struct NULL = off.  The scaled logit is logit * (1 / temperature),
- * both rounded to fp32; temperature <= 0 keeps the most likely token (the first of equals) only.  Tokens are ordered by
+ * both rounded to fp32 and at most its largest finite number in magnitude (an infinite logit is that at every temperature); temperature <= 0 or NaN keeps the most likely token (the first of equals) only.  Tokens are ordered by
  * scaled logit, equals by index.  top_k <= 0 or >= V is off; top_p >= 1 is off, and the most likely token is kept whatever it is;
  * min_p <= 0 is off, more than 1 counts as 1.  They apply in turn: the top_k first tokens; of these the shortest prefix with at least
  * top_p of their probability; of these all at least min_p times as likely as the likeliest.

@@ -728,13 +728,15 @@ struct CatRequest {   // what the caller asks of a row
   __device__ __forceinline__ CatRequest(const CatParams& p, int64_t r) {
     const float temp = p.temperature ? p.temperature[r] : 1.0f;
     const bool greedy = !(temp > 0.0f);
-    inv_t = greedy ? 1.0f : __fdiv_rn(1.0f, temp);
+    inv_t = greedy ? 1.0f : fminf(__fdiv_rn(1.0f, temp), FLT_MAX);   // (of a subnormal temperature: 0 times it has to be 0)
     want = greedy ? 1 : (p.top_k ? p.top_k[r] : 0);
     if (want <= 0 || want >= p.V) want = 0;
     top_p = p.top_p ? p.top_p[r] : 1.0f;
     by_p = top_p < 1.0f && !greedy;
     few = want > 0 && want <= kCatTau;
   }
+  // Scaled logits have to be numbers: at an infinite temperature they are 0, but an infinite one stays beyond the range, as at every other temperature.
+  __device__ __forceinline__ void at_top(float largest) { if (inv_t == 0.0f && largest == INFINITY) inv_t = __uint_as_float(1u); }
 };
 // The least scaled logit that min-p keeps: the smallest fp32 number not below m + log(min_p).
 __device__ __forceinline__ float cat_least(const CatParams& p, int64_t r, float m) {
@@ -1265,11 +1267,12 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
   const int64_t r = p.r0 + row_i;
   constexpr int kVec = CatRow<T>::kVec;
   griddep_enter();
-  const CatRequest q(p, r);
+  CatRequest q(p, r);
   const CatRow<T> row(p.logits, r, p.V);
   if (tid == 0) sh.list_n = 0;
   cat_table(sh.tab);
   const CatTop top = cat_tops(sh, p.w, row_i);
+  q.at_top(cat_key_value(static_cast<u64>(top.top) << 32));
   if (top.live == 0) {   // nothing is left
     if (split == 0 && tid == 0) {
       if (p.dist) { double* d = p.dist + r * kCatRow; d[0] = -INFINITY; d[1] = INFINITY; d[2] = -1.0; d[3] = 0.0; d[4] = q.inv_t; }
@@ -1339,11 +1342,12 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_
   CatState* st = p.w.state + row_i;
   const int mode = st->mode;
   if (mode == CAT_DONE || (mode == CAT_SEARCH && split > 0)) return;
-  const CatRequest q(p, r);
+  CatRequest q(p, r);
   const CatRow<T> row(p.logits, r, p.V);
   if (tid == 0) sh.list_n = 0;
   cat_table(sh.tab);
   const CatTop top = cat_tops(sh, p.w, row_i);
+  q.at_top(cat_key_value(static_cast<u64>(top.top) << 32));
   const float m = cat_scale(cat_key_value(static_cast<u64>(top.top) << 32), q.inv_t);
   const bool by_k = q.want > 0 && static_cast<uint32_t>(q.want) < top.live;
   u64* seg = p.w.seg + static_cast<int64_t>(row_i) * p.w.pieces;
@@ -1386,7 +1390,7 @@ __global__ void __launch_bounds__(NB, 1024 / NB) cat_row_kernel(const __grid_con
   const int64_t r = p.r0 + blockIdx.x;
   constexpr int kVec = CatRow<T>::kVec, kU = NB >= 1024 ? 4 : 8;
   griddep_enter();
-  const CatRequest q(p, r);
+  CatRequest q(p, r);
   const CatRow<T> from(p.logits, r, p.V);
   const CatHeld<T> row{data, from.head, p.V, (from.head + p.V + kVec - 1) / kVec};
   cat_table(sh.tab);
@@ -1421,6 +1425,8 @@ __global__ void __launch_bounds__(NB, 1024 / NB) cat_row_kernel(const __grid_con
     live = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(x));
     low = __reduce_max_sync(0xffffffffu, lane < NB / 32 ? static_cast<uint32_t>(sh.red[lane][1]) : 0u);
   }
+  const float raw_m = cat_key_value(static_cast<u64>(top) << 32);
+  q.at_top(raw_m);
   if (live == 0) {   // nothing is left
     if (tid == 0) {
       if (p.dist) { double* d = p.dist + r * kCatRow; d[0] = -INFINITY; d[1] = INFINITY; d[2] = -1.0; d[3] = 0.0; d[4] = q.inv_t; }
@@ -1428,7 +1434,7 @@ __global__ void __launch_bounds__(NB, 1024 / NB) cat_row_kernel(const __grid_con
     }
     return;
   }
-  const float raw_m = cat_key_value(static_cast<u64>(top) << 32), m = cat_scale(raw_m, q.inv_t);
+  const float m = cat_scale(raw_m, q.inv_t);
   const bool by_k = q.want > 0 && static_cast<uint32_t>(q.want) < live;
   const int pieces = row.pieces();
   const CatScale sc(m, kCatFloor);

@@ -634,3 +634,30 @@ def test_infinite_and_overflowing_logits_at_the_top(R, V, dtype):
                 for r in rng.integers(0, R, 2):
                     assert np.array_equal(d[r, 1:], _cat.kept(_f32(l[r:r + 1])[0], **g)[2][1:]), (r, g, d[r])
     ctx.close()
+
+
+@pytest.mark.parametrize("R,V", [(2, 1000), (400, 33001), (3, 100003)])
+def test_temperatures_at_the_ends_of_their_range(R, V):
+    """A subnormal temperature, whose reciprocal is beyond fp32, and an infinite one beside an infinite logit: what is 0 stays 0, what is infinite infinite."""
+    ctx = _ctx()
+    u = _dev(np.full(R, 0.5, np.float32))
+    fmax, T = np.finfo(np.float32).max, float(np.float32(1e-40))
+    x = np.full((R, V), -1.0, np.float32)
+    x[:, 4] = 0.0; x[:, 9] = -np.inf; x[:, V - 3] = -1e-40
+    for f in (dict(), dict(top_k=1), dict(top_k=3), dict(top_k=500), dict(top_p=0.6), dict(top_k=500, top_p=0.6), dict(min_p=0.9)):
+        tok, lp, d = _sample(ctx, _dev(x), u, _params([dict(temperature=T, **f)] * R), R, V)
+        low = np.float32(np.float32(-1e-40) * fmax)         # (about -0.03)
+        z = 1 + np.exp(np.float64(low))
+        kept = {0: V - 1, 1: 1, 3: 3, 500: 500}[f.get("top_k", 0)]
+        n = min(kept, 2) if "top_p" in f or "min_p" in f else kept
+        assert np.all(d[:, 4] == fmax) and np.all(d[:, 3] == n), (f, d[0])
+        if n == 1:
+            assert np.all(tok == 4) and np.all(lp == 0) and np.all(d[:, 0] == 0)
+        else:
+            assert np.all(tok == 4) and np.all(np.abs(d[:, 0] - np.log(z)) < _border(V)) and np.all(d[:, 1] == (low if n == 2 else -fmax))
+    x = np.zeros((R, V), np.float32)
+    x[:, 7] = np.inf; x[:, 3] = -np.inf; x[:, 5] = np.nan; x[:, 11] = fmax
+    for f, n in ((dict(), V - 2), (dict(top_k=1), 1), (dict(top_k=3), 3), (dict(top_k=500), 500), (dict(top_p=0.9), 1), (dict(top_k=500, top_p=0.9), 1), (dict(min_p=0.5), 1)):
+        tok, lp, d = _sample(ctx, _dev(x), u, _params([dict(temperature=np.inf, **f)] * R), R, V)
+        assert np.all(tok == 7) and np.all(lp == 0) and np.all(d[:, 3] == n) and np.all(d[:, 0] == fmax), (f, d[0], tok[0], lp[0])
+    ctx.close()
