@@ -661,3 +661,129 @@ def test_temperatures_at_the_ends_of_their_range(R, V):
         tok, lp, d = _sample(ctx, _dev(x), u, _params([dict(temperature=np.inf, **f)] * R), R, V)
         assert np.all(tok == 7) and np.all(lp == 0) and np.all(d[:, 3] == n) and np.all(d[:, 0] == fmax), (f, d[0], tok[0], lp[0])
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_parts_of_a_row_and_one_block_give_the_same_bits(dtype):
+    """A row of 45001 alone (many parts), in a batch of 30 (one block that holds it) and of 400 (three kernels, one part), rows on and off 16 bytes."""
+    rng = np.random.default_rng(22)
+    V = 45001
+    wide = _dev((rng.standard_normal((1, V + 3)) * 1.5).astype(np.float32), TYPES[dtype])
+    u = np.array([0.613], np.float32)
+    ctx = _ctx()
+    for off in (0, 1, 3):
+        x = wide[:, off:off + V]
+        for f in (dict(), dict(top_p=0.9), dict(top_k=40), dict(top_k=4000, top_p=0.8), dict(top_k=200, top_p=0.95, min_p=0.01), dict(top_k=300), dict(min_p=0.05), dict(temperature=0.0)):
+            f = {"temperature": 0.9, **f}
+            one = _sample(ctx, x, _dev(u), _params([f]), 1, V)
+            _check_rows(_f32(x), *one, u, [f])
+            for R in (5, 30, 400):
+                many = _sample(ctx, x.expand(R, -1), _dev(np.repeat(u, R)), _params([f] * R), R, V)
+                for a, b in zip(one, many):
+                    assert np.all(b == a[0]), (f, off, R)
+    ctx.close()
+
+
+def test_more_rows_than_a_group():
+    """1500 rows go in two groups that share the workspace, each row with filters of its own: the bits of calls of 100 rows (one block a row)."""
+    R, V = 1500, 20011
+    rng = np.random.default_rng(23)
+    x = torch.randn(R, V, generator=torch.Generator("cuda").manual_seed(1), device="cuda") * 2
+    x[::7, 100:9000] = -np.inf
+    fs = [[dict(), dict(top_p=0.9), dict(top_k=20), dict(top_k=1500, top_p=0.7), dict(min_p=0.02), dict(temperature=0.0), dict(top_k=100, top_p=0.9, min_p=0.01)][r % 7 if r % 5 else 1]
+          for r in range(R)]
+    fs = [{"temperature": float(np.float32(rng.uniform(0.6, 1.4))), **f} for f in fs]
+    u = rng.random(R).astype(np.float32)
+    ctx = _ctx()
+    tok, lp, d = _sample(ctx, x, _dev(u), _params(fs), R, V)
+    for r in range(0, R, 100):
+        for a, b in zip(_sample(ctx, x[r:r + 100], _dev(u[r:r + 100]), _params(fs[r:r + 100]), 100, V), (tok, lp, d)):
+            assert np.array_equal(a, b[r:r + 100]), r
+    at = [0, 1, 2, 3, 4, 5, 6, 749, 750, 751, 752, 753, 754, 1498, 1499]
+    _check_rows(_f32(x[at]), tok[at], lp[at], d[at], u[at], [fs[i] for i in at])
+    ctx.close()
+
+
+def test_more_sequences_than_a_group():
+    """5000 sequences are resampled in two groups: the tokens of calls of 1000."""
+    B, V = 5000, 515
+    g = torch.Generator("cuda").manual_seed(2)
+    p, q = torch.randn(2 * B, V, generator=g, device="cuda") * 2, torch.randn(B, V, generator=g, device="cuda") * 2
+    dp, dq = torch.zeros(2 * B, 5, dtype=torch.float64, device="cuda"), torch.zeros(B, 5, dtype=torch.float64, device="cuda")
+    n = torch.randint(3, (B,), generator=g, device="cuda").to(torch.int32)     # (2: out of range)
+    w = torch.rand(B, generator=g, device="cuda")
+    ctx = _ctx()
+    ctx.csd_cat_filter(2 * B, V, p, None, dp)
+    ctx.csd_cat_filter(B, V, q, None, dq)
+    new, part = (torch.full((B,), 9999, dtype=torch.int32, device="cuda") for _ in range(2))
+    for _ in range(2):                                                          # tickets are zero again after a call
+        ctx.csd_cat_resample(B, 1, 2, V, q, dq, p, dp, n, w, new)
+    for b in range(0, B, 1000):
+        e = b + 1000
+        ctx.csd_cat_resample(1000, 1, 2, V, q[b:e], dq[b:e], p[2 * b:2 * e], dp[2 * b:2 * e], n[b:e], w[b:e], part[b:e])
+    ctx.sync()
+    assert torch.equal(new, part) and torch.equal(new == -1, n == 2)
+    hp, hq = p.view(B, 2, V).cpu().numpy(), q.cpu().numpy()
+    for b in (0, 1, 2, 3, 4095, 4096, 4097, 4998, 4999):
+        j = int(n[b])
+        if j < 2:
+            r = _cat.probabilities(hp[b, j])[0]
+            if j == 0:
+                r = np.maximum(r - _cat.probabilities(hq[b])[0], 0.0)
+            want, near = _cat.pick(r, float(w[b]))
+            assert int(new[b]) == want or near < (2.0 ** -41 + V * 2.0 ** -53) / r.sum()
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_long_16_bit_rows_with_top_k_and_top_p(dtype):
+    """Many parts a row, many equals: top-k ends in a bin of its own behind top-p's, before it, and in the same one."""
+    R, V = 4, 100003
+    rng = np.random.default_rng(24)
+    x = 2 * rng.standard_normal((R, V))
+    x[:, rng.integers(0, V, 40)] += 5
+    l = _dev(x.astype(np.float32), TYPES[dtype])
+    u = rng.random(R).astype(np.float32)
+    ctx = _ctx()
+    for k, p, mp in ((3000, 0.5, 0.0), (1000, 0.9, 0.0), (300, 0.999, 0.0), (20000, 0.6, 0.0), (5000, 0.3, 0.004), (700, 0.7, 0.05)):
+        fs = [dict(temperature=float(np.float32(t)), top_k=k + i, top_p=float(np.float32(p)), min_p=float(np.float32(mp))) for i, t in enumerate((1.0, 0.7, 1.2, 0.9))]
+        _check_rows(_f32(l), *_sample(ctx, l, _dev(u), _params(fs), R, V), u, fs)
+    ctx.close()
+
+
+def test_workspaces_that_grow_leave_captured_calls_their_own():
+    """A graph of small calls, then larger calls of the same context (its buffers are replaced), then the graph again, and small calls."""
+    from paper_2411_11925_b200 import api
+    rng = np.random.default_rng(25)
+    s = torch.cuda.Stream()
+    ctx, plain = api.Context(0, s), _ctx()
+
+    def inputs(B, gamma, V):
+        f = lambda *sh: _dev((rng.standard_normal(sh) * 2).astype(np.float32))  # noqa: E731
+        u = lambda *sh: _dev(rng.random(sh).astype(np.float32))  # noqa: E731
+        return (f(B * gamma, V), f(B * (gamma + 1), V), None, None, u(B * gamma), u(B, gamma), u(B), B, gamma, gamma + 1, V)
+
+    small, large = inputs(2, 2, 70001), inputs(30, 4, 80001)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        _round(ctx, *small)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            out = _round(ctx, *small)
+        big = _round(ctx, *large)                 # larger in rows, parts and sums
+        g.replay()
+        again = _round(ctx, *small)
+        big2 = _round(ctx, *large)
+        for o in out:
+            o.fill_(-3)
+        g.replay()
+    torch.cuda.synchronize()
+    want, want_big = _round(plain, *small), _round(plain, *large)
+    plain.sync()
+    for a, b, c in zip(out, again, want):
+        assert torch.equal(a, c) and torch.equal(b, c)
+    for a, b, c in zip(big, big2, want_big):
+        assert torch.equal(a, c) and torch.equal(b, c)
+    ctx.sync()
+    del g
+    ctx.close(); plain.close()

@@ -316,3 +316,40 @@ def test_vocabulary_head_round_captured():
             assert int(new[b]) == x or near < 1e-10 / r.sum()
     del g
     ctx.close()
+
+
+@pytest.mark.parametrize("M,N,K,dtype", [(230, 30001, 700, "bf16"), (96, 60001, 300, "f32"), (70, 20000, 1200, "f16")])
+def test_products_of_several_tiles_a_pair_of_blocks(M, N, K, dtype):
+    """More tiles than pairs of blocks: accumulators, stages and groups of scales are used again, at odd numbers of column blocks too."""
+    g = torch.Generator("cuda").manual_seed(K)
+    ctx = _ctx()
+    a = torch.randn(M, K, generator=g, device="cuda") * torch.exp2(torch.randint(-3, 4, (M, 1), generator=g, device="cuda").float())
+    w = torch.randn(N, K, generator=g, device="cuda") * K ** -0.5 * torch.exp2(torch.randint(-3, 4, (N, 1), generator=g, device="cuda").float())
+    a[:, 128:256] *= 64
+    qa, qw = _quant(ctx, a), _quant(ctx, w)
+    out = torch.full((M, N + 3), 3.0, device="cuda", dtype=TYPES[dtype])
+    ctx.csd_quant_matmul(M, N, K, qa, qw, out[:, 1:1 + N])
+    again = torch.zeros(M, N, device="cuda", dtype=TYPES[dtype])
+    ctx.csd_quant_matmul(M, N, K, qa, qw, again)
+    ctx.sync()
+    fa, fw = (torch.from_numpy(_cat.dequantize(*(t.cpu().numpy() for t in q))).cuda() for q in (qa, qw))
+    want, size = fa @ fw.T, fa.abs() @ fw.abs().T
+    tol = K * 2.0 ** -23 * size + HALF_STEP[dtype] * want.abs() + (2.0 ** -25 if dtype == "f16" else 0.0)
+    assert torch.all((out[:, 1:1 + N].double() - want).abs() <= tol) and torch.equal(out[:, 1:1 + N], again)
+    assert torch.all(out[:, 0] == 3) and torch.all(out[:, 1 + N:] == 3)
+    ctx.close()
+
+
+def test_quantize_below_the_least_scale():
+    """Blocks whose scale would lie below 2^-127 get that: the least normal number is 2 in it, the least subnormal one rounds to 0."""
+    x = torch.zeros(2, 256, device="cuda")
+    x[0, 0] = 2.0 ** -126; x[0, 128] = 1.5
+    x[1, :128] = 2.0 ** -149
+    ctx = _ctx()
+    q = _quant(ctx, x)
+    ctx.sync()
+    s = q[1].cpu().numpy()
+    got = _cat.dequantize(q[0].cpu().numpy(), s)
+    assert s[0, 0] == 0 and s[0, 1] == 119 and s[1, 0] == 0
+    assert got[0, 0] == 2.0 ** -126 and got[0, 128] == 1.5 and np.all(got[0, 1:128] == 0) and np.all(got[1] == 0)
+    ctx.close()
