@@ -787,3 +787,113 @@ def test_workspaces_that_grow_leave_captured_calls_their_own():
     ctx.sync()
     del g
     ctx.close(); plain.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_largest_vocabulary(dtype):
+    """2^19 tokens, rows on and off 16 bytes (one piece more): equals throughout (sums next to 2^63), flat rows, peaks; sampling and resampling."""
+    V = 1 << 19
+    rng = np.random.default_rng(26)
+    wide = torch.zeros(3, V + 9, dtype=TYPES[dtype], device="cuda")
+    u = np.array([0.25, 0.9999999, 0.5], np.float32)
+    ctx = _ctx()
+    for off in (0, 1, 7):
+        x = wide[:, off:off + V]
+        x.zero_()
+        x[1] = _dev(1.5 * rng.standard_normal(V).astype(np.float32), TYPES[dtype])
+        x[2] = _dev(2 * rng.standard_normal(V).astype(np.float32), TYPES[dtype])
+        x[2, [5, V // 2, V - 1]] = 25.0
+        h = _f32(x)
+        for f in (dict(), dict(top_p=0.9), dict(top_k=100), dict(top_k=300000)):
+            fs = [{"temperature": 1.0, **f}] * 3
+            tok, lp, d = _sample(ctx, x, _dev(u), _params(fs), 3, V)
+            _check_rows(h[1:], tok[1:], lp[1:], d[1:], u[1:], fs[1:])
+            n = f.get("top_k", V) if "top_p" not in f else int(np.ceil(np.float64(np.float32(0.9)) * V))
+            # (equals: weights of 2^44 and a few units, all the same)
+            assert d[0, 3] == n and d[0, 2] == n - 1 and d[0, 1] == 0 and abs(d[0, 0] - np.log(n)) < 1e-15 * 20 and tok[0] == int(np.ceil(0.25 * n)) - 1
+        q = torch.zeros(3, V, device="cuda")
+        dq, dp = (torch.zeros(3, 5, dtype=torch.float64, device="cuda") for _ in range(2))
+        new = torch.full((3,), -5, dtype=torch.int32, device="cuda")
+        ctx.csd_cat_filter(3, V, q, None, dq)
+        ctx.csd_cat_filter(3, V, x, None, dp)
+        ctx.csd_cat_resample(3, 1, 1, V, q, dq, x, dp, torch.zeros_like(new), _dev(u), new)
+        ctx.sync()
+        for b in range(3):
+            p, _ = _cat.probabilities(h[b])
+            r = np.maximum(p - 1.0 / V, 0.0)
+            r = p if b == 0 else r
+            want, near = _cat.pick(r, u[b])
+            assert int(new[b]) == want or near < (2.0 ** -41 + V * 2.0 ** -53) / r.sum(), (off, b, int(new[b]), want)
+    ctx.close()
+
+
+def test_many_short_rows():
+    R, V = 200000, 5
+    g = torch.Generator("cuda").manual_seed(3)
+    x, u = torch.randn(R, V, generator=g, device="cuda"), torch.rand(R, generator=g, device="cuda").clamp(1e-6, 1 - 1e-6)
+    ctx = _ctx()
+    tok, lp, d = _sample(ctx, x, u, None, R, V)
+    p = torch.softmax(x.double(), 1)
+    c = torch.cumsum(p, 1)
+    want = (c < u.double()[:, None] * c[:, -1:]).sum(1)
+    near = (c - u.double()[:, None]).abs().amin(1) < 1e-12
+    tok = torch.from_numpy(tok).cuda().long()
+    assert torch.all((tok == want) | near)
+    assert torch.all((torch.from_numpy(lp).cuda().double() - torch.log(p.gather(1, tok[:, None])[:, 0])).abs() < 1e-6)
+    assert np.all(d[:, 3] == V)
+    ctx.close()
+
+
+@pytest.mark.parametrize("at_p,at_q", [(5000.0, 5000.0), (1e6, 0.0), (0.0, -1e6), (-3e38, 1e30)])
+def test_resampling_of_large_logits(at_p, at_q):
+    """Normalisers so large that a difference from them has to be formed with care, of p, of q, of both: the residual of the rows as they round."""
+    B, gamma, V = 6, 2, 3001
+    rng = np.random.default_rng(27)
+    p = (2 * rng.standard_normal((B, gamma + 1, V)) + at_p).astype(np.float32)
+    q = (2 * rng.standard_normal((B * gamma, V)) + at_q).astype(np.float32)
+    u0, u, w = rng.random(B * gamma).astype(np.float32), rng.random((B, gamma)).astype(np.float32), rng.random(B).astype(np.float32).clip(1e-6)
+    ctx = _ctx()
+    tok, dq, dp, lr, n, mask, new = _round(ctx, _dev(q), _dev(p.reshape(-1, V)), None, None, _dev(u0), _dev(u), _dev(w), B, gamma, gamma + 1, V)
+    for j in range(gamma + 1):
+        n.fill_(j)
+        ctx.csd_cat_resample(B, gamma, gamma + 1, V, _dev(q), dq, _dev(p.reshape(-1, V)), dp, n, _dev(w), new)
+        ctx.sync()
+        for b in range(B):
+            r, _ = _cat.probabilities(p[b, j])
+            if j < gamma:
+                rest = np.maximum(r - _cat.probabilities(q[b * gamma + j])[0], 0.0)
+                r = rest if rest.sum() > 0 else r
+            want, near = _cat.pick(r, w[b])
+            # (a summary is rounded to fp64: 2^-53 of the normaliser, in the exponent)
+            assert int(new[b]) == want or near < (2.0 ** -40 + 2.0 ** -52 * (abs(at_p) if abs(at_p) < 1e7 else 0) + V * 2.0 ** -53) / r.sum(), (b, j)
+    ctx.close()
+
+
+def test_two_contexts_on_two_streams_at_once():
+    from paper_2411_11925_b200 import api
+    rng = np.random.default_rng(28)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ctxs, plain = [api.Context(0, s) for s in streams], _ctx()
+    args = []
+    for k in range(2):
+        B, gamma, V = 20 + 30 * k, 3, 60001
+        f = lambda *sh: _dev((rng.standard_normal(sh) * 2).astype(np.float32))  # noqa: E731
+        u = lambda *sh: _dev(rng.random(sh).astype(np.float32))  # noqa: E731
+        fp = _params([dict(temperature=0.9, top_k=[0, 50, 4000][r % 3], top_p=0.9) for r in range(B * (gamma + 1))])
+        args.append((f(B * gamma, V), f(B * (gamma + 1), V), None, fp, u(B * gamma), u(B, gamma), u(B), B, gamma, gamma + 1, V))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(_round(ctxs[k], *args[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        want = _round(plain, *args[k])
+        plain.sync()
+        for out in got[k]:
+            for a, b in zip(out, want):
+                assert torch.equal(a, b)
+    for c in ctxs + [plain]:
+        c.sync()
+        c.close()

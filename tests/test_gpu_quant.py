@@ -353,3 +353,31 @@ def test_quantize_below_the_least_scale():
     assert s[0, 0] == 0 and s[0, 1] == 119 and s[1, 0] == 0
     assert got[0, 0] == 2.0 ** -126 and got[0, 128] == 1.5 and np.all(got[0, 1:128] == 0) and np.all(got[1] == 0)
     ctx.close()
+
+
+@pytest.mark.parametrize("rows,K,dtype,off", [(3, 8200, "bf16", 0), (3, 9001, "bf16", 1), (5, 16384, "f16", 0), (2, 12003, "f16", 3), (300, 8193, "bf16", 0), (2, 16392, "bf16", 0), (3, 20001, "f32", 1)])
+def test_norm_of_wide_rows_in_place(rows, K, dtype, off):
+    """Rows of four pieces a thread, and rows that are read twice, on and off 16 bytes; the sum replaces the residual, or x, or both where they are one array."""
+    rng = np.random.default_rng(K)
+    t = lambda *sh: torch.from_numpy(rng.standard_normal(sh).astype(np.float32)).cuda().to(TYPES[dtype])  # noqa: E731
+    w = t(K)
+    ctx = _ctx()
+    for which in ("residual", "x", "both"):
+        bx, br = t(rows, K + 8), t(rows, K + 8)
+        x = bx[:, off:off + K]
+        r = x if which == "both" else br[:, off:off + K]
+        keep = bx.clone(), br.clone()
+        h = x.double() + r.double()
+        rounded = (x.float() + r.float()).to(TYPES[dtype])
+        y = h / torch.sqrt((h ** 2).mean(1, keepdim=True) + 1e-5) * w.double()
+        q = _empty(rows, K)
+        ctx.csd_norm_quantize(rows, K, x, r, w, 1e-5, x if which == "x" else r, *q)
+        ctx.sync()
+        # fp32: as in test_norm_quantize, rows read twice have K / 1024 more terms in a thread
+        _check_bytes(q, y.cpu().numpy(), 2.0 ** -24 * ((K / 256 + 20) / 2 + 2 + 2 + 3), K)
+        assert torch.equal(x if which != "residual" else r, rounded)
+        for buf, was in zip((bx, br), keep):                   # nothing beside the rows, and not the other array
+            same = buf == was
+            same[:, off:off + K] |= torch.equal(buf[:, off:off + K], rounded)
+            assert torch.all(same)
+    ctx.close()
