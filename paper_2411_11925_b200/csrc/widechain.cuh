@@ -322,7 +322,7 @@ __device__ __forceinline__ bool wc_poll(ulonglong2 (&w)[8], const ulonglong2* a,
       "mov.u64 now, %%clock64;\n\tshr.u64 now, now, 10;\n\tcvt.u32.u64 x, now;\n\tsub.u32 x, x, t0;\n\t"
       "setp.lt.u32 p, x, 64;\n\t@p bra AGAIN;\n\t"                                           // (the limit is read only then)
       "cvt.u64.u32 now, x;\n\t"
-      "ld.volatile.global.u64 most, [%23];\n\tshr.u64 most, most, 10;\n\t"
+      "ld.volatile.global.u64 most, [%23];\n\tshr.u64 most, most, 10;\n\tadd.u64 most, most, 1;\n\t"   // (both ends are rounded down: never before the limit)
       "setp.le.u64 p, now, most;\n\t@p bra AGAIN;\n\t"
       "mov.u32 %16, 1;\n"
       "DONE:\n\t}"
