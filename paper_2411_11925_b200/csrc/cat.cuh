@@ -344,6 +344,7 @@ template <int NT> struct CatShared {
   CatState state;                             // of a row that one block holds
   // found by one thread, read by all
   u64 found_key, found_sum, found_upto, found_before[2];
+  double norm;
   uint32_t found_n;
   int found_a, found_b, found_k, found_prev, found_listed, found_piece;
   float found_lo, found_hi;
@@ -878,15 +879,19 @@ __device__ __forceinline__ u64 cat_keep(const R& row, int p0, int p1, u64* seg, 
 template <int NT, typename R>
 __device__ __forceinline__ void cat_finish(CatShared<NT>& sh, const CatParams& p, int64_t r, const R& row, const u64* seg, float inv_t, const CatScale& sc, float m, const CatKept& kept) {
   const int tid = threadIdx.x;
-  // The sum in units of the largest token's own weight: 2^44 but for the rounding of CatScale's c, which all weights share and the quotient takes
-  // out.  A token that is certain has the quotient 1, so the normaliser is its scaled logit and its log probability 0, exactly.
-  const double norm = static_cast<double>(m) + log(static_cast<double>(kept.w) / static_cast<double>(cat_weight(m, sc, sh.tab)));
   const CatBound bound{cat_key_value(kept.last), static_cast<int>(static_cast<uint32_t>(kept.last))};
-  if (tid == 0 && p.dist) {
-    double* d = p.dist + r * kCatRow;
-    d[0] = norm; d[1] = bound.value; d[2] = bound.idx; d[3] = static_cast<double>(kept.n); d[4] = inv_t;
-  }
-  if (!p.u) return;
+  auto summary = [&] {   // by a thread of the warp that has least to do
+    if (tid != NT - 1) return;
+    // The sum in units of the largest token's own weight: 2^44 but for the rounding of CatScale's c, which all weights share and the quotient takes
+    // out.  A token that is certain has the quotient 1, so the normaliser is its scaled logit and its log probability 0, exactly.
+    const double norm = static_cast<double>(m) + log(static_cast<double>(kept.w) / static_cast<double>(cat_weight(m, sc, sh.tab)));
+    sh.norm = norm;
+    if (p.dist) {
+      double* d = p.dist + r * kCatRow;
+      d[0] = norm; d[1] = bound.value; d[2] = bound.idx; d[3] = static_cast<double>(kept.n); d[4] = inv_t;
+    }
+  };
+  if (!p.u) return summary();
   const u64 target = cat_target(p.u[r], kept.w);
   int found = -1;
   if (kept.listed == static_cast<int>(kept.n) && kept.listed <= NT) {   // all of them are listed: each adds up those of smaller index
@@ -896,6 +901,7 @@ __device__ __forceinline__ void cat_finish(CatShared<NT>& sh, const CatParams& p
     const u64 own = tid < n ? cat_weight(cat_key_value(sh.list[tid]), sc, sh.tab) : 0;
     w[tid] = own;
     cat_sync<NT>();
+    summary();
     if (tid < n) {
       const uint32_t idx = static_cast<uint32_t>(sh.list[tid]);
       u64 before = 0;
@@ -903,6 +909,7 @@ __device__ __forceinline__ void cat_finish(CatShared<NT>& sh, const CatParams& p
       if (before < target && before + own >= target) found = static_cast<int>(idx);
     }
   } else {
+    summary();
     found = cat_locate(sh, row, seg, target, kept.listed, [&](u64 key) { return cat_weight(cat_key_value(key), sc, sh.tab); },
                        [&](const float* l, int idx, u64* w) {
 #pragma unroll
@@ -913,9 +920,14 @@ __device__ __forceinline__ void cat_finish(CatShared<NT>& sh, const CatParams& p
       }
     });
   }
+  if (!p.logp) {
+    if (found >= 0) p.token[r] = found;
+    return;
+  }
+  cat_sync<NT>();                             // the normaliser is known
   if (found >= 0) {
     p.token[r] = found;
-    if (p.logp) p.logp[r] = static_cast<float>(static_cast<double>(cat_scale(cat_float(row.at(found)), inv_t)) - norm);
+    p.logp[r] = static_cast<float>(static_cast<double>(cat_scale(cat_float(row.at(found)), inv_t)) - sh.norm);
   }
 }
 
