@@ -17,8 +17,8 @@
 // conclusion for the row.  One kernel that kept a row in a cluster took 2 to 4 times as long: its passes shared 64 registers with
 // everything a row's state needs, and a reduction through distributed shared memory cost 1.3 us.
 //
-// Bound by instructions, not by reading: 52 a token with its weight (11 of them fp64), 24 a token counted.  512 rows of 131072 fp32 with top-p take
-// 304 us (the three kernels 47, 104 and 160; reading once at the copy rate 41), 576 of 65536 bf16 with top-k 200 and top-p, with the ratios, 68 (reading 12).
+// Bound by instructions, not by reading: 47 a token with its weight (11 of them fp64), 22 a token counted.  512 rows of 131072 fp32 with top-p take
+// 306 us (the three kernels, each alone, 49, 92 and 175; reading once at the copy rate 41), 576 of 65536 bf16 with top-k 200 and top-p, with the ratios, 68 (reading 12).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -965,7 +965,7 @@ __device__ __noinline__ void cat_search(CatShared<NT>& sh, const CatParams& p, i
 // ------------------------------------------------------------------------------------------------------------- kernels
 // The largest logit of a part (scaling is monotonic: the largest scaled one is its scaled logit) and how many are not masked; for a
 // small top-k also a threshold above which that many tokens of the row lie for certain: this part's share of them, by its threads' own maxima.
-// Bound by reading the logits (512 x 131072 fp32 in 47 us, 5.7 TB/s).
+// Bound by reading the logits (512 x 131072 fp32 in 49 us, 5.5 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(kCatThreads) cat_top_kernel(const __grid_constant__ CatParams p) {
   __shared__ uint2 part[kCatWarps];
@@ -1346,7 +1346,7 @@ __global__ void __launch_bounds__(kCatThreads, 4) cat_scan_kernel(const __grid_c
 
 // What cat_scan_kernel left: the weights above the bins in question (all weights where top-p refers to the whole row), piece by
 // piece, and the tokens of those bins, of which the row's last block derives the cut.  Bound by instructions:
-// 52 a token, two thirds of the issue slots taken, the fp64 pipe to 28 % (a third of the time is dependent fp64 steps at 32 warps an SM).
+// 47 a token, 62 % of the issue slots taken, the fp64 pipe to 30 % (a third of the time is dependent fp64 steps at 32 warps an SM).
 template <typename T>
 __global__ void __launch_bounds__(kCatThreads, 4) cat_range_kernel(const __grid_constant__ CatParams p) {
   __shared__ CatShared<kCatThreads> sh;

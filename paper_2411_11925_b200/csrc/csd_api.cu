@@ -1522,9 +1522,9 @@ int cat_filter(csd_ctx* ctx, int64_t R, int V, const csd_logits* l, const csd_ca
   if (R > ctx->num_sms && by256) return launch_cat_row<256>(ctx, l->dtype, p, R, by256);
   if (R > ctx->num_sms && by512) return launch_cat_row<512>(ctx, l->dtype, p, R, by512);
   if (by1024 && R <= ctx->num_sms && (R > 16 || V <= 40000)) return launch_cat_row<1024>(ctx, l->dtype, p, R, by1024);
-  // Rows go in groups whose workspace is bounded (32 KB a row).  Groups small enough for L2 to hold their logits from one kernel to
+  // Rows go in groups whose workspace is bounded (a row: 32 KB of counts and candidates, 8 B a piece, 40 B a part).  Groups small enough for L2 to hold their logits from one kernel to
   // the next took longer: the passes are not bound by reading, and each group's kernels fill and drain the device once more (512 rows of
-  // 131072 fp32 logits with top-p 0.92: 512 us in groups of 64 MB, 332 in one).
+  // 131072 fp32 logits with top-p 0.92: 512 us in groups of 64 MB, 332 in one, which takes 306 by now).
   int64_t group = R < 1024 ? R : 1024;
   const int64_t groups = (R + group - 1) / group;
   group = (R + groups - 1) / groups;

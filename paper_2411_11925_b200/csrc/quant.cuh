@@ -41,7 +41,7 @@ template <> __device__ __forceinline__ __half quant_from_float<__half>(float v) 
 
 // Eight elements of a row from column `col` on as they lie, zeros behind the row's end.  16-bit rows that are not 16-byte aligned
 // are read as aligned vectors too, one more than the elements fill, and shifted (element by element a warp's loads touch every line eight
-// times: 154 us against 117 at 8192 x 5001 bf16 with residual; fp32, 216 and 236, goes by element); so do not pieces that would reach beyond the row.
+// times: 154 us against 117 at 8192 x 5001 bf16 with residual; fp32, where the two were 216 and 236 side by side, goes by element: 234 as the kernel stands); so do not pieces that would reach beyond the row.
 template <typename T> struct QuantRaw { __align__(16) T e[8]; };
 // VEC: K is a multiple of 8 and rows are 16-byte aligned, a piece is a whole one or none.
 template <bool VEC, typename T>
@@ -165,7 +165,7 @@ __device__ __forceinline__ uint2 quant_pack8(const float* v, uint32_t byte) {
 template <typename T, int NCH> constexpr int quant_rows_resident() { return NCH == 1 || NCH == 2 ? 2 : 1; }
 
 // A block takes rows blockIdx.x, + gridDim.x, ...: the next row is requested before this one's reduction, so that its reads are under
-// way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, 64 as it is;
+// way while the block waits and writes (one block a row, without that: 79 us at 8192 x 5000 bf16 with residual, 63 as it is;
 // 288 MB take 44 us at the rate of a copy, instructions bound 16-bit rows: 8192 x 4096 fp32 go at 6.4 TB/s, bf16 at 4.8).  A thread holds NCH pieces of eight columns (NCH = 0: rows too wide for that are read
 // twice), 16 lanes a scale block.  Sums and the norm in fp32; the sum leaves rounded to the input's type, the norm uses it unrounded.
 template <typename T, int NCH, bool NORM, bool VEC>
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(NCH > 0 ? 512 : 1024, quant_rows_resident<T, N
 //   warps 2..5  bring the scales into tensor memory, a word (four blocks) per row: row 32 j + i at lane i, column j, in all
 //               four lane quarters; the token rows' scales into both blocks'
 //   warps 6..   epilogue: a lane is a vocabulary row, a register a token.  (Two tokens' columns packed to words by an exchange between lanes, for
-//               half as many stores, took 119 us where this takes 90: 576 x 65536 x 2048, bf16)
+//               half as many stores, took 119 us where the kernel without it took 90: 576 x 65536 x 2048, bf16, which takes 79 in a short run, 94 under the power cap)
 struct QuantMmaParams {
   int M, N, nkb, ls;          // token rows, vocabulary rows, blocks of 128 columns, scale bytes a row
   int bn, stages, sf_col, tmem_cols, tiles_m, tiles;
@@ -291,7 +291,7 @@ struct QuantMmaParams {
   void* out;
   int64_t ldo;
 };
-constexpr int kQmEpi = 8;       // epilogue warps (with four the MMAs waited for them where the sums are short: 576 x 65536 x 2048 101 us, 93)
+constexpr int kQmEpi = 8;       // epilogue warps (with four the MMAs waited for them where the sums are short: 576 x 65536 x 2048 under the power cap 101 us, 94)
 constexpr int kQmThreads = 32 * (6 + kQmEpi);
 constexpr int kQmABytes = 128 * kQuantBlock;
 constexpr int kQmSfCols = 12;   // 4 of the weights' scales, up to 8 of the tokens'
